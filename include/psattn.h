@@ -326,6 +326,95 @@ psattn_status psattn_split_planes(const float* X, void* planes, int64_t n, void*
 psattn_status psattn_silu_bwd(const float* dM_planes, const void* A, const void* B, void* dA_planes, void* dB_planes,
                               int64_t n, void* stream);
 
+/* ---- The rest of a training step behind the layers: the loss over the vocabulary and the weights' update. */
+
+/* Log-probabilities of next tokens over a vocabulary, and their gradient, without the logits in memory:
+ *   z[r][v] = logit_scale * X[r] . W[v],  LSE[r] = log sum_v exp z[r][v],
+ *   logp[e] = z[r][tgt[e]] - LSE[r]   for the targets e = tgt_ptr[r] .. tgt_ptr[r+1]-1 of row r.
+ * X [rows][hidden] (the last layer's rows, normalised), W [vocab][hidden], of one dtype, row-major, 16-byte aligned; hidden
+ * a multiple of 8.  Targets are lists by row because a shared row can have several next tokens: the last row of a node the
+ * first token of every child, a masked row none.  tgt_ptr [rows+1] int32 ascending from 0 to targets (values outside
+ * 0 .. targets are taken as the nearest one), tgt [targets] int32.  A target outside 0 .. vocab-1 is left out: its logp is
+ * 0 and it has no gradient.  The same target may be listed more than once.  rows and targets may be 0 (pointers
+ * to nothing may then be NULL). */
+typedef struct {
+  int64_t rows;          /* < 2^31 */
+  int64_t targets;       /* < 2^31 */
+  int32_t hidden;        /* multiple of 8, at most 2^20 */
+  int32_t vocab;         /* >= 1, at most 2^30 */
+  float logit_scale;     /* > 0, finite; 1 / sampling temperature */
+  psattn_dtype dtype;    /* of X, W, dX and dW */
+} psattn_logprob_desc;
+
+/* Workspace bytes for pass 0 (psattn_logprob_fwd) or 1 (psattn_logprob_bwd). */
+psattn_status psattn_logprob_workspace_size(const psattn_logprob_desc* desc, int pass, size_t* bytes);
+/* logp [targets] and LSE [rows], fp32. */
+psattn_status psattn_logprob_fwd(const psattn_logprob_desc* desc, const void* X, const void* W, const int32_t* tgt_ptr,
+                                 const int32_t* tgt, float* logp, float* LSE, void* ws, size_t ws_bytes, void* stream);
+/* Gradients for the adjoints dlogp [targets] (fp32) of logp.  With p = exp(z - LSE) and G[r] the sum of row r's dlogp:
+ *   dz[r][v] = sum of dlogp[e] over r's targets equal to v  -  G[r] p[r][v]
+ *   dX[r] = logit_scale * sum_v dz[r][v] W[v],   dW[v] = logit_scale * sum_r dz[r][v] X[r].
+ * A row without a target of non-zero dlogp has dX 0 and no part in dW, whatever its X and LSE hold.  dX [rows][hidden]
+ * and dW [vocab][hidden] are of the desc's dtype and overwritten; either may be NULL if it is not wanted.  The logits are
+ * computed again, a piece of the vocabulary at a time.  bf16: dz is rounded once to bf16, sums are fp32.  fp32: every
+ * product is formed from bf16 planes (psattn_split_planes) and holds fp32 precision; a non-finite X or W
+ * makes the results that it enters NaN.  Sums have a fixed order: results are bitwise repeatable. */
+psattn_status psattn_logprob_bwd(const psattn_logprob_desc* desc, const void* X, const void* W, const int32_t* tgt_ptr,
+                                 const int32_t* tgt, const float* LSE, const float* dlogp, void* dX, void* dW, void* ws,
+                                 size_t ws_bytes, void* stream);
+
+/* AdamW over many tensors at once.  For each element, with g = s * grad:
+ *   m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,
+ *   w <- w (1 - lr weight_decay decay) - lr / (1 - b1^step) * m / (sqrt(v) / sqrt(1 - b2^step) + eps)
+ * in fp32.  s = grad_scale, times min(1, max_norm / (norm + 1e-6)) where max_norm > 0, with norm the 2-norm of all
+ * grad_scale * grad, summed in fp64 in a fixed order; where that norm is not finite, the step changes nothing.
+ * Without max_norm a non-finite gradient makes its own element non-finite and no other.
+ * state_bits 32: m and v fp32.  state_bits 8: m and r = sqrt(v) as e4m3 codes, with a byte per 256 elements (the
+ * block's power of two, biased by 127) such that the block's largest finite magnitude has a code in [128, 256].  A value
+ * between two codes takes the upper one at random, with a probability in proportion to its place between them, by 16 bits of a hash
+ * of (seed, step, tensor, element): rounded to the nearest, an average whose changes are smaller than half a code
+ * would never move.  A positive r is never rounded to 0, which keeps m / r bounded. */
+typedef struct {
+  void* param;           /* [n] bf16 or fp32 */
+  float* master;         /* bf16: the fp32 weights [n], of which param is the rounded copy.  fp32: NULL */
+  void* m;               /* [n] fp32, or e4m3 codes */
+  void* v;               /* [n] fp32, or the e4m3 codes of sqrt(v) */
+  uint8_t* m_exp;        /* state_bits 8: [(n + 255) / 256], else NULL */
+  uint8_t* v_exp;
+  int64_t n;             /* elements, >= 1 */
+  float decay;           /* factor of weight_decay (0: none, as for norms), >= 0 */
+  psattn_dtype dtype;    /* of param */
+} psattn_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;   /* >= 0; betas < 1; eps > 0 */
+  double max_norm;       /* 0: no clipping */
+  double grad_scale;     /* usually 1 */
+  int64_t step;          /* 1 for the first */
+  uint32_t seed;         /* of the random rounding (state_bits 8) */
+  uint32_t reserved;     /* must be 0 */
+} psattn_adamw_hyper;
+/* The values that change from step to step, in device memory (16-byte aligned): where given, they stand for those of the
+ * hyper struct, so that a captured step can be replayed with new ones. */
+typedef struct {
+  float lr, grad_scale;
+  int32_t step;          /* values below 1 count as 1 */
+  uint32_t seed;
+} psattn_adamw_dyn;
+typedef struct psattn_adamw psattn_adamw;
+
+/* Host only.  Pointers are device pointers, 16-byte aligned; no two buffers may overlap (PSATTN_E_INVALID_ARG). */
+psattn_status psattn_adamw_create(int32_t num_tensors, const psattn_adamw_tensor* tensors, int32_t state_bits, psattn_adamw** out);
+void psattn_adamw_destroy(psattn_adamw* opt);
+/* Device memory for the tensors' table (caller-owned, 256-byte aligned), and its upload as for a tree. */
+psattn_status psattn_adamw_device_bytes(const psattn_adamw* opt, size_t* bytes);
+psattn_status psattn_adamw_upload(psattn_adamw* opt, void* dev_buf, size_t bytes, void* stream);
+psattn_status psattn_adamw_workspace_size(const psattn_adamw* opt, size_t* bytes);
+/* One step.  grads [num_tensors] (a host array of device pointers, 16-byte aligned; NULL: that tensor is left as it is),
+ * grad_dtypes [num_tensors]; dyn (device, optional); grad_norm (device, optional, one fp32: the norm before clipping). */
+psattn_status psattn_adamw_step(const psattn_adamw* opt, const void* const* grads, const int32_t* grad_dtypes,
+                                const psattn_adamw_hyper* hyper, const psattn_adamw_dyn* dyn, float* grad_norm, void* ws,
+                                size_t ws_bytes, void* stream);
+
 /* Reference count of every node: the number of samples whose path holds it
  * (Sec. 5.2).  node_refcount has num_nodes entries. */
 psattn_status psattn_tree_refcounts(const psattn_tree* tree, int32_t* node_refcount);

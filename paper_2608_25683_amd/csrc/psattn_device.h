@@ -420,5 +420,38 @@ __device__ __forceinline__ bool row_dq(float (&dq)[D / 64], float& sum, const bo
   return true;
 }
 
+// ---- fp32 tensors as three bf16 planes, for products with a bf16 tensor on the bf16 matrix cores.
+// x = x1 + x2 + x3 exactly: each plane takes the next 8 bits of x's 24-bit significand (truncation, so
+// that nothing overflows; infinities and NaN stay in x1).  The product of a plane and a bf16 number is
+// exact in fp32, so three bf16 products with fp32 sums hold what one fp32 product holds.
+__device__ __forceinline__ void split3(float x, uint32_t& x1, uint32_t& x2, uint32_t& x3) {
+  const uint32_t u = __float_as_uint(x);
+  const bool special = (u & 0x7f800000u) == 0x7f800000u;
+  const uint32_t h = (u & 0xffff0000u) | (special && (u & 0x007fffffu) ? 0x00400000u : 0u);
+  const float r = special ? 0.f : x - __uint_as_float(u & 0xffff0000u);
+  const uint32_t m = __float_as_uint(r) & 0xffff0000u;
+  const float l = r - __uint_as_float(m);
+  x1 = h >> 16;
+  x2 = m >> 16;
+  x3 = __float_as_uint(l) >> 16;
+}
+
+// four consecutive elements into the three planes (n elements each) at element i
+__device__ __forceinline__ void put_planes(const f32x4& x, bf16_t* y, int64_t n, int64_t i) {
+  uint32_t p[3][4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) split3(x[k], p[0][k], p[1][k], p[2][k]);
+#pragma unroll
+  for (int j = 0; j < 3; ++j) *(u32x2*)(y + j * n + i) = u32x2{p[j][0] | p[j][1] << 16, p[j][2] | p[j][3] << 16};
+}
+
+// (VEC: n is a multiple of 4, four elements per lane and turn; else one)
+__device__ __forceinline__ void put_plane1(float x, bf16_t* y, int64_t n, int64_t i) {
+  uint32_t p[3];
+  split3(x, p[0], p[1], p[2]);
+#pragma unroll
+  for (int j = 0; j < 3; ++j) y[j * n + i] = (bf16_t)p[j];
+}
+
 }  // namespace dev
 }  // namespace psattn

@@ -1076,8 +1076,11 @@ struct Profiler {
 };
 Profiler g_prof;
 const char* kKernelNames[] = {"fwd_main", "fwd_merge",     "bwd_pre", "bwd_kv",   "bwd_dq", "bwd_reduce_kv",
-                              "bwd_reduce_dq", "rope",       "kv_scatter", "kv_gather", "split_planes", "silu_bwd"};
-constexpr int kNumKernels = 12;
+                              "bwd_reduce_dq", "rope",       "kv_scatter", "kv_gather", "split_planes", "silu_bwd",
+                              "logprob_prep", "logprob_wplanes", "logprob_logits", "logprob_finish", "logprob_dz", "logprob_dx",
+                              "logprob_dx_sum", "logprob_dw", "adamw_norm", "adamw_scalars", "adamw_step"};
+constexpr int kNumKernels = 23;
+enum { K_LP_PREP = 12, K_LP_WPLANES, K_LP_LOGITS, K_LP_FINISH, K_LP_DZ, K_LP_DX, K_LP_DX_SUM, K_LP_DW, K_ADAMW_NORM, K_ADAMW_SCALARS, K_ADAMW_STEP };
 
 hipEvent_t get_event() {
   if (!g_prof.spare.empty()) {
@@ -1323,6 +1326,333 @@ psattn_status psattn_silu_bwd(const float* dM_planes, const void* A, const void*
     return fail(PSATTN_E_ALIGNMENT, "tensor pointers must be 16-byte aligned");
   hipStream_t st = (hipStream_t)stream;
   return timed(11, st, [&] { return launch_silu_bwd(dM_planes, A, B, dA_planes, dB_planes, n, st); });
+}
+
+// ---------------------------------------------------------------------------------------------
+// Log-probabilities over a vocabulary
+
+}  // extern "C"
+
+namespace {
+
+int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
+
+// Everything of the arguments that follows from the sizes, and the workspace: buffers as offsets.
+struct LogprobPlan {
+  LogprobArgs a{};
+  size_t part = 0, total = 0, xc = 0, wc = 0, dl = 0, dx_acc = 0, bytes = 0;
+};
+
+psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& p) {
+  if (!d) return fail(PSATTN_E_INVALID_ARG, "desc is NULL");
+  if (pass != 0 && pass != 1) return fail(PSATTN_E_INVALID_ARG, "pass must be 0 or 1 (got %d)", pass);
+  if (d->dtype != PSATTN_BF16 && d->dtype != PSATTN_FP32) return fail(PSATTN_E_UNSUPPORTED, "unknown dtype %d", (int)d->dtype);
+  if (d->rows < 0 || d->rows > INT32_MAX - 1024) return fail(PSATTN_E_INVALID_ARG, "rows %lld outside 0 .. 2^31 - 1025", (long long)d->rows);
+  if (d->targets < 0 || d->targets > INT32_MAX) return fail(PSATTN_E_INVALID_ARG, "targets %lld outside 0 .. 2^31 - 1", (long long)d->targets);
+  if (d->hidden < 8 || d->hidden % 8 || d->hidden > 1 << 20)
+    return fail(PSATTN_E_UNSUPPORTED, "hidden %d: a multiple of 8, 8 .. 2^20, is needed", d->hidden);
+  if (d->vocab < 1 || d->vocab > 1 << 30) return fail(PSATTN_E_INVALID_ARG, "vocab %d outside 1 .. 2^30", d->vocab);
+  if (!(d->logit_scale > 0.f) || !std::isfinite(d->logit_scale)) return fail(PSATTN_E_INVALID_ARG, "logit_scale must be finite and > 0");
+  LogprobArgs& a = p.a;
+  const bool fp32 = d->dtype == PSATTN_FP32, bwd = pass == 1;
+  a.n = (int32_t)d->rows;
+  a.h = d->hidden;
+  a.v = d->vocab;
+  a.e = (int32_t)d->targets;
+  a.planes = fp32 ? 3 : 1;
+  a.hp = (int32_t)up64(a.h);
+  a.np = (int32_t)up64(a.n);
+  a.scale = d->logit_scale;
+  // A piece's dz (backward) and the planes of its weights (fp32) stay under 512 MiB: on 8192 rows that is 32768 entries, and
+  // the fp32 sums of dX, which every piece but the last reads and writes, are a twentieth of its traffic.
+  const int64_t vr = (a.v + 255) / 256, per = 256 * 2 * (int64_t)a.planes;
+  int64_t cap = vr;
+  if (bwd && a.np) cap = std::min<int64_t>(cap, ((int64_t)512 << 20) / (per * a.np));
+  if (fp32) cap = std::min<int64_t>(cap, ((int64_t)512 << 20) / (per * a.hp));
+  cap = std::max<int64_t>(cap, 1);
+  a.pieces = (int32_t)((vr + cap - 1) / cap);
+  const int64_t each = (vr + a.pieces - 1) / a.pieces;
+  a.pieces = (int32_t)((vr + each - 1) / each);
+  a.piece_v = (int32_t)(256 * each);
+  a.splits = 1;
+  size_t cur = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = cur;
+    cur = align_up(cur + bytes);
+    return at;
+  };
+  const bool copy = bwd || fp32 || a.h != a.hp;
+  if (copy) p.xc = take((size_t)a.planes * a.np * a.hp * 2);
+  if (fp32) p.wc = take((size_t)a.planes * a.piece_v * a.hp * 2);
+  if (!bwd) {
+    p.part = take((size_t)((a.v + LP_PART - 1) / LP_PART) * a.n * sizeof(LogprobStat));
+  } else {
+    p.total = take((size_t)a.n * 4);
+    p.dl = take((size_t)a.planes * a.np * a.piece_v * 2);
+    if (a.pieces > 1 || a.splits > 1) p.dx_acc = take((size_t)a.splits * a.n * a.h * 4);
+  }
+  p.bytes = cur;
+  return PSATTN_OK;
+}
+
+// The checks that both passes share, and the pointers into the workspace.
+psattn_status logprob_begin(const psattn_logprob_desc* d, int pass, const void* X, const void* W, const int32_t* tgt_ptr,
+                            const int32_t* tgt, void* ws, size_t ws_bytes, LogprobPlan& p) {
+  psattn_status s = logprob_plan(d, pass, p);
+  if (s != PSATTN_OK) return s;
+  LogprobArgs& a = p.a;
+  if (!W || !tgt_ptr || (a.n && !X) || (a.e && !tgt)) return fail(PSATTN_E_INVALID_ARG, "NULL argument");
+  if (misaligned(X) || misaligned(W)) return fail(PSATTN_E_ALIGNMENT, "X and W must be 16-byte aligned");
+  if (((uintptr_t)tgt_ptr | (uintptr_t)tgt) & 3) return fail(PSATTN_E_ALIGNMENT, "tgt_ptr and tgt must be 4-byte aligned");
+  if (p.bytes > ws_bytes || (p.bytes && !ws))
+    return fail(PSATTN_E_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, p.bytes);
+  if (p.bytes && misaligned(ws)) return fail(PSATTN_E_ALIGNMENT, "workspace must be 16-byte aligned");
+  if (!launch_logprob_logits) return fail(PSATTN_E_HIP, "built without the kernels of psattn_logprob.hip");
+  a.X = X;
+  a.W = W;
+  a.tgt_ptr = tgt_ptr;
+  a.tgt = tgt;
+  char* b = (char*)ws;
+  a.part = (LogprobStat*)(b + p.part);
+  a.total = (float*)(b + p.total);
+  const bool copy = pass == 1 || a.planes == 3 || a.h != a.hp;
+  a.xc = copy ? (uint16_t*)(b + p.xc) : nullptr;
+  a.wc = a.planes == 3 ? (uint16_t*)(b + p.wc) : nullptr;
+  a.dl = (uint16_t*)(b + p.dl);
+  a.dx_acc = a.pieces > 1 || a.splits > 1 ? (float*)(b + p.dx_acc) : nullptr;
+  return PSATTN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+psattn_status psattn_logprob_workspace_size(const psattn_logprob_desc* desc, int pass, size_t* bytes) {
+  if (!bytes) return fail(PSATTN_E_INVALID_ARG, "NULL argument");
+  LogprobPlan p;
+  const psattn_status s = logprob_plan(desc, pass, p);
+  if (s == PSATTN_OK) *bytes = p.bytes;
+  return s;
+}
+
+psattn_status psattn_logprob_fwd(const psattn_logprob_desc* desc, const void* X, const void* W, const int32_t* tgt_ptr,
+                                 const int32_t* tgt, float* logp, float* LSE, void* ws, size_t ws_bytes, void* stream) {
+  LogprobPlan p;
+  psattn_status s = logprob_begin(desc, 0, X, W, tgt_ptr, tgt, ws, ws_bytes, p);
+  if (s != PSATTN_OK) return s;
+  LogprobArgs& a = p.a;
+  if ((a.e && !logp) || (a.n && !LSE)) return fail(PSATTN_E_INVALID_ARG, "NULL argument");
+  if (((uintptr_t)logp | (uintptr_t)LSE) & 3) return fail(PSATTN_E_ALIGNMENT, "logp and LSE must be 4-byte aligned");
+  a.logp = logp;
+  a.lse_out = LSE;
+  if (!a.n) return PSATTN_OK;
+  hipStream_t st = (hipStream_t)stream;
+  if (a.xc) s = timed(K_LP_PREP, st, [&] { return launch_logprob_prep(a, false, st); });
+  for (int i = 0; i < a.pieces && s == PSATTN_OK; ++i) {
+    if (a.wc) s = timed(K_LP_WPLANES, st, [&] { return launch_logprob_wplanes(a, i, st); });
+    if (s == PSATTN_OK) s = timed(K_LP_LOGITS, st, [&] { return launch_logprob_logits(a, i, false, st); });
+  }
+  if (s == PSATTN_OK) s = timed(K_LP_FINISH, st, [&] { return launch_logprob_finish(a, st); });
+  return s;
+}
+
+psattn_status psattn_logprob_bwd(const psattn_logprob_desc* desc, const void* X, const void* W, const int32_t* tgt_ptr,
+                                 const int32_t* tgt, const float* LSE, const float* dlogp, void* dX, void* dW, void* ws,
+                                 size_t ws_bytes, void* stream) {
+  LogprobPlan p;
+  psattn_status s = logprob_begin(desc, 1, X, W, tgt_ptr, tgt, ws, ws_bytes, p);
+  if (s != PSATTN_OK) return s;
+  LogprobArgs& a = p.a;
+  if ((a.e && !dlogp) || (a.n && !LSE)) return fail(PSATTN_E_INVALID_ARG, "NULL argument");
+  if (((uintptr_t)dlogp | (uintptr_t)LSE) & 3) return fail(PSATTN_E_ALIGNMENT, "dlogp and LSE must be 4-byte aligned");
+  if (misaligned(dX) || misaligned(dW)) return fail(PSATTN_E_ALIGNMENT, "dX and dW must be 16-byte aligned");
+  a.lse = LSE;
+  a.dlogp = dlogp;
+  a.dX = a.n ? dX : nullptr;
+  a.dW = dW;
+  if (!a.dX && !a.dW) return PSATTN_OK;
+  hipStream_t st = (hipStream_t)stream;
+  if (a.n) s = timed(K_LP_PREP, st, [&] { return launch_logprob_prep(a, true, st); });
+  for (int i = 0; i < a.pieces && s == PSATTN_OK; ++i) {
+    if (a.n && a.wc) s = timed(K_LP_WPLANES, st, [&] { return launch_logprob_wplanes(a, i, st); });
+    if (s == PSATTN_OK && a.n) s = timed(K_LP_DZ, st, [&] { return launch_logprob_logits(a, i, true, st); });
+    if (s == PSATTN_OK && a.dX) s = timed(K_LP_DX, st, [&] { return launch_logprob_dx(a, i, st); });
+    if (s == PSATTN_OK && a.dW) s = timed(K_LP_DW, st, [&] { return launch_logprob_dw(a, i, st); });
+  }
+  if (s == PSATTN_OK && a.dX && a.splits > 1) s = timed(K_LP_DX_SUM, st, [&] { return launch_logprob_dx_sum(a, st); });
+  return s;
+}
+
+// ---------------------------------------------------------------------------------------------
+// AdamW over many tensors
+
+}  // extern "C"
+
+struct psattn_adamw {
+  std::vector<AdamwTensor> tensors;
+  std::vector<AdamwItem> items;       // tensor by tensor
+  std::vector<int64_t> first_item;    // of each tensor, and the end
+  int32_t bits = 32;
+  size_t o_items = 0, bytes = 0;
+  void* dev = nullptr;
+};
+
+namespace {
+
+size_t adamw_workspace(const psattn_adamw* o) { return kAlign + o->items.size() * sizeof(double); }
+
+psattn_status adamw_create(int32_t n, const psattn_adamw_tensor* ts, int32_t bits, psattn_adamw& o) {
+  struct Range { uintptr_t lo, hi; int32_t tensor; };
+  std::vector<Range> held;
+  o.bits = bits;
+  for (int32_t i = 0; i < n; ++i) {
+    const psattn_adamw_tensor& t = ts[i];
+    if (t.dtype != PSATTN_BF16 && t.dtype != PSATTN_FP32) return fail(PSATTN_E_UNSUPPORTED, "tensor %d: unknown dtype %d", i, (int)t.dtype);
+    const bool bf16 = t.dtype == PSATTN_BF16;
+    if (t.n < 1 || t.n > (int64_t)1 << 40) return fail(PSATTN_E_INVALID_ARG, "tensor %d: n %lld outside 1 .. 2^40", i, (long long)t.n);
+    if (!t.param || !t.m || !t.v) return fail(PSATTN_E_INVALID_ARG, "tensor %d: NULL argument", i);
+    if (bf16 != (t.master != nullptr)) return fail(PSATTN_E_INVALID_ARG, "tensor %d: bf16 weights have a master, fp32 weights none", i);
+    if ((bits == 8) != (t.m_exp != nullptr) || (bits == 8) != (t.v_exp != nullptr))
+      return fail(PSATTN_E_INVALID_ARG, "tensor %d: m_exp and v_exp belong to 8-bit states", i);
+    if (!(t.decay >= 0.f) || !std::isfinite(t.decay)) return fail(PSATTN_E_INVALID_ARG, "tensor %d: decay must be finite and >= 0", i);
+    if (misaligned(t.param) || misaligned(t.master) || misaligned(t.m) || misaligned(t.v))
+      return fail(PSATTN_E_ALIGNMENT, "tensor %d: pointers must be 16-byte aligned", i);
+    auto hold = [&](const void* p, int64_t bytes) {
+      if (p) held.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, i});
+    };
+    const int64_t state = t.n * (bits == 8 ? 1 : 4), exps = (t.n + ADAMW_BLOCK - 1) / ADAMW_BLOCK;
+    hold(t.param, t.n * (bf16 ? 2 : 4));
+    hold(t.master, t.n * 4);
+    hold(t.m, state);
+    hold(t.v, state);
+    hold(t.m_exp, exps);
+    hold(t.v_exp, exps);
+    o.tensors.push_back({t.param, t.master, t.m, t.v, t.m_exp, t.v_exp, t.n, t.decay, bf16 ? 1 : 0});
+    o.first_item.push_back((int64_t)o.items.size());
+    const int64_t chunks = (t.n + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
+    if ((int64_t)o.items.size() + chunks > 1 << 30) return fail(PSATTN_E_UNSUPPORTED, "tensor %d: more than 2^43 elements in all", i);
+    for (int64_t c = 0; c < chunks; ++c) o.items.push_back({i, (int32_t)c});
+  }
+  o.first_item.push_back((int64_t)o.items.size());
+  std::sort(held.begin(), held.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
+  for (size_t k = 1; k < held.size(); ++k)
+    if (held[k].lo < held[k - 1].hi)
+      return fail(PSATTN_E_INVALID_ARG, "buffers of tensors %d and %d overlap", held[k - 1].tensor, held[k].tensor);
+  o.o_items = align_up(o.tensors.size() * sizeof(AdamwTensor));
+  o.bytes = align_up(o.o_items + o.items.size() * sizeof(AdamwItem));
+  return PSATTN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+psattn_status psattn_adamw_create(int32_t num_tensors, const psattn_adamw_tensor* tensors, int32_t state_bits, psattn_adamw** out) {
+  if (!out) return fail(PSATTN_E_INVALID_ARG, "out is NULL");
+  if (num_tensors < 1 || !tensors) return fail(PSATTN_E_INVALID_ARG, "no tensors");
+  if (state_bits != 8 && state_bits != 32) return fail(PSATTN_E_UNSUPPORTED, "state_bits %d: 8 or 32", state_bits);
+  psattn_adamw* o = nullptr;
+  try {
+    o = new psattn_adamw;
+    const psattn_status s = adamw_create(num_tensors, tensors, state_bits, *o);
+    if (s == PSATTN_OK) *out = o;
+    else delete o;
+    return s;
+  } catch (const std::exception& e) {
+    delete o;
+    return fail(PSATTN_E_INVALID_ARG, "the tensors' table does not fit in host memory: %s", e.what());
+  }
+}
+
+void psattn_adamw_destroy(psattn_adamw* opt) { delete opt; }
+
+psattn_status psattn_adamw_device_bytes(const psattn_adamw* o, size_t* bytes) {
+  if (!o || !bytes) return fail(PSATTN_E_INVALID_ARG, "NULL argument");
+  *bytes = o->bytes;
+  return PSATTN_OK;
+}
+
+psattn_status psattn_adamw_upload(psattn_adamw* o, void* dev_buf, size_t bytes, void* stream) {
+  if (!o || !dev_buf) return fail(PSATTN_E_INVALID_ARG, "NULL argument");
+  if (((uintptr_t)dev_buf & (kAlign - 1)) != 0) return fail(PSATTN_E_ALIGNMENT, "table buffer must be 256-byte aligned");
+  if (bytes < o->bytes) return fail(PSATTN_E_WORKSPACE, "table buffer of %zu bytes, %zu needed", bytes, o->bytes);
+  hipStream_t st = (hipStream_t)stream;
+  hipError_t e = hipMemcpyAsync(dev_buf, o->tensors.data(), o->tensors.size() * sizeof(AdamwTensor), hipMemcpyHostToDevice, st);
+  if (e == hipSuccess)
+    e = hipMemcpyAsync((char*)dev_buf + o->o_items, o->items.data(), o->items.size() * sizeof(AdamwItem), hipMemcpyHostToDevice, st);
+  if (e == hipSuccess) e = hipStreamSynchronize(st);
+  if (e != hipSuccess) return fail(PSATTN_E_HIP, "table upload failed: %s", hipGetErrorString(e));
+  o->dev = dev_buf;
+  return PSATTN_OK;
+}
+
+psattn_status psattn_adamw_workspace_size(const psattn_adamw* o, size_t* bytes) {
+  if (!o || !bytes) return fail(PSATTN_E_INVALID_ARG, "NULL argument");
+  *bytes = adamw_workspace(o);
+  return PSATTN_OK;
+}
+
+psattn_status psattn_adamw_step(const psattn_adamw* o, const void* const* grads, const int32_t* grad_dtypes,
+                                const psattn_adamw_hyper* h, const psattn_adamw_dyn* dyn, float* grad_norm, void* ws,
+                                size_t ws_bytes, void* stream) {
+  if (!o || !grads || !grad_dtypes || !h) return fail(PSATTN_E_INVALID_ARG, "NULL argument");
+  if (!o->dev) return fail(PSATTN_E_NOT_UPLOADED, "call psattn_adamw_upload before psattn_adamw_step");
+  auto nonneg = [](double x) { return x >= 0 && std::isfinite(x); };
+  if (!nonneg(h->lr) || !nonneg(h->weight_decay) || !nonneg(h->max_norm)) return fail(PSATTN_E_INVALID_ARG, "lr, weight_decay and max_norm must be finite and >= 0");
+  if (!nonneg(h->beta1) || !(h->beta1 < 1) || !nonneg(h->beta2) || !(h->beta2 < 1)) return fail(PSATTN_E_INVALID_ARG, "betas must lie in [0, 1)");
+  if (!(h->eps > 0) || !std::isfinite(h->eps)) return fail(PSATTN_E_INVALID_ARG, "eps must be finite and > 0");
+  if (!std::isfinite(h->grad_scale)) return fail(PSATTN_E_INVALID_ARG, "grad_scale must be finite");
+  if (h->step < 1 || h->step > INT32_MAX) return fail(PSATTN_E_INVALID_ARG, "step %lld outside 1 .. 2^31 - 1", (long long)h->step);
+  if (h->reserved) return fail(PSATTN_E_INVALID_ARG, "reserved must be 0");
+  if (misaligned(dyn)) return fail(PSATTN_E_ALIGNMENT, "dyn must be 16-byte aligned");
+  if ((uintptr_t)grad_norm & 3) return fail(PSATTN_E_ALIGNMENT, "grad_norm must be 4-byte aligned");
+  const size_t need = adamw_workspace(o);
+  if (!ws || ws_bytes < need) return fail(PSATTN_E_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? ws_bytes : (size_t)0, need);
+  if (misaligned(ws)) return fail(PSATTN_E_ALIGNMENT, "workspace must be 16-byte aligned");
+  const int32_t n = (int32_t)o->tensors.size();
+  for (int32_t i = 0; i < n; ++i) {
+    if (grad_dtypes[i] != PSATTN_BF16 && grad_dtypes[i] != PSATTN_FP32) return fail(PSATTN_E_UNSUPPORTED, "gradient %d: unknown dtype %d", i, grad_dtypes[i]);
+    if (misaligned(grads[i])) return fail(PSATTN_E_ALIGNMENT, "gradient %d must be 16-byte aligned", i);
+  }
+  if (!launch_adamw_step) return fail(PSATTN_E_HIP, "built without the kernels of psattn_adamw.hip");
+  hipStream_t st = (hipStream_t)stream;
+  AdamwArgs a{};
+  a.tensors = (const AdamwTensor*)o->dev;
+  a.items = (const AdamwItem*)((const char*)o->dev + o->o_items);
+  a.total_items = (int32_t)o->items.size();
+  a.bits = o->bits;
+  a.dev_out = (AdamwScalars*)ws;
+  a.part = (double*)((char*)ws + kAlign);
+  a.dyn = dyn;
+  a.norm = grad_norm;
+  a.hyper = *h;
+  const bool with_norm = h->max_norm > 0 || grad_norm;
+  // the launches of a pass over the elements: groups of ADAMW_GRADS tensors, whose pointers are arguments
+  auto pass = [&](int kernel, hipError_t (*launch)(const AdamwArgs&, const AdamwGrads&, hipStream_t)) {
+    psattn_status s = PSATTN_OK;
+    for (int32_t t0 = 0; t0 < n && s == PSATTN_OK; t0 += ADAMW_GRADS) {
+      const int32_t t1 = std::min(n, t0 + ADAMW_GRADS);
+      AdamwGrads g{};
+      for (int32_t i = t0; i < t1; ++i) {
+        g.g[i - t0] = grads[i];
+        if (grad_dtypes[i] == PSATTN_BF16) g.bf16[(i - t0) / 32] |= 1u << ((i - t0) % 32);
+      }
+      a.tensor0 = t0;
+      a.item0 = (int32_t)o->first_item[t0];
+      a.n_items = (int32_t)(o->first_item[t1] - o->first_item[t0]);
+      s = timed(kernel, st, [&] { return launch(a, g, st); });
+    }
+    return s;
+  };
+  psattn_status s = PSATTN_OK;
+  if (with_norm) s = pass(K_ADAMW_NORM, launch_adamw_norm);
+  if (s == PSATTN_OK && (with_norm || dyn)) {
+    s = timed(K_ADAMW_SCALARS, st, [&] { return launch_adamw_scalars(a, with_norm, st); });
+    a.dev = a.dev_out;
+  }
+  if (!a.dev) a.s = adamw_scalars(a.hyper, a.hyper.lr, a.hyper.grad_scale, a.hyper.step, a.hyper.seed);
+  if (s == PSATTN_OK) s = pass(K_ADAMW_STEP, launch_adamw_step);
+  return s;
 }
 
 psattn_status psattn_tree_refcounts(const psattn_tree* t, int32_t* node_refcount) {

@@ -145,3 +145,102 @@ class SharedLayer:
         dhh = dh * f(W["g1"])
         dX = dy + (dhh - xn * (dhh * xn).mean(-1, keepdim=True)) * s["r1"]
         return dX, g
+
+
+def row_targets(parent, seg_len, row_off, tokens):
+    """The next tokens of every shared row, as lists by row: (tgt_ptr [Ns + 1], tgt, entry [Ns]), int32 numpy arrays, for
+    psattn_logprob_fwd.  A row inside a node has one, the node's next token; a node's last row has the first token of
+    each of its children (in node order), none at a leaf.  tokens [Ns]: the token of each row.  entry[r] is the list entry
+    that predicts row r's token, -1 where no row of this call does (a root's first token, and that of a node behind a
+    cached one)."""
+    parent, seg_len, row_off, tokens = (np.asarray(x) for x in (parent, seg_len, row_off, tokens))
+    ns = int(seg_len[row_off >= 0].sum())
+    if tokens.shape != (ns,):
+        raise ValueError(f"expected {ns} tokens, got {tokens.shape}")
+    src = np.full(ns, -1, dtype=np.int64)         # the row behind which each row's token comes
+    for n in range(len(parent)):
+        a = int(row_off[n])
+        if a < 0:
+            continue
+        src[a + 1:a + int(seg_len[n])] = np.arange(a, a + int(seg_len[n]) - 1)
+        p = int(parent[n])
+        if p >= 0 and row_off[p] >= 0:
+            src[a] = int(row_off[p]) + int(seg_len[p]) - 1
+    first = np.asarray([int(a) for a in row_off if a >= 0], dtype=np.int64)
+    node_rank = np.zeros(ns, dtype=np.int64)      # order among the rows behind one row: that of their nodes
+    node_rank[first] = np.arange(len(first))
+    dst = np.flatnonzero(src >= 0)
+    dst = dst[np.lexsort((node_rank[dst], src[dst]))]
+    ptr = np.zeros(ns + 1, dtype=np.int32)
+    ptr[1:] = np.cumsum(np.bincount(src[dst], minlength=ns))
+    entry = np.full(ns, -1, dtype=np.int32)
+    entry[dst] = np.arange(len(dst))
+    return ptr, tokens[dst].astype(np.int32), entry
+
+
+def advantage_dlogp(parent, seg_len, row_off, sample_end, adv: Sequence[float],
+                    loss_mask: Callable[[int, np.ndarray], np.ndarray], entry: np.ndarray) -> np.ndarray:
+    """Adjoint of the log-probabilities for the loss -sum_s A_s sum_t m_{s,t} logp(token t of sample s): a shared token collects
+    the terms of every sample that holds it (Sec. 2.5, Sec. 4.1.1).  loss_mask as for advantage_adjoint; entry is row_targets'."""
+    parent, seg_len, row_off = np.asarray(parent), np.asarray(seg_len), np.asarray(row_off)
+    w = np.zeros(int(entry.max(initial=-1)) + 1)
+    for s, e in enumerate(sample_end):
+        path = []
+        n = int(e)
+        while n >= 0:
+            path.append(n)
+            n = int(parent[n])
+        rows = np.concatenate([np.arange(int(row_off[m]), int(row_off[m]) + int(seg_len[m])) for m in reversed(path) if row_off[m] >= 0])
+        m = np.asarray(loss_mask(s, rows), dtype=np.float64)
+        known = entry[rows] >= 0
+        w[entry[rows][known]] -= float(adv[s]) * m[known]
+    return w
+
+
+class SharedHead:
+    """What follows the last layer: h = rmsnorm(x) g, and the log-probabilities of each shared row's next tokens over the
+    vocabulary (psattn_logprob_fwd / _bwd).  Weights W: g [H], W [V, H]."""
+
+    def __init__(self, W: Dict[str, "torch.Tensor"], logit_scale: float = 1.0, eps: float = 1e-6):
+        self.W, self.scale, self.eps = W, logit_scale, eps
+
+    def forward(self, X, tgt_ptr, tgt):
+        """logp [targets] (fp32) and what the backward needs."""
+        import torch
+        r = torch.rsqrt(X.float().pow(2).mean(-1, keepdim=True) + self.eps)
+        h = (X.float() * r).to(X.dtype) * self.W["g"]
+        logp, lse = P.psattn_logprob_fwd(h, self.W["W"], tgt_ptr, tgt, logit_scale=self.scale)
+        return logp, dict(X=X, r=r, h=h, lse=lse, tgt_ptr=tgt_ptr, tgt=tgt)
+
+    def backward(self, saved, dlogp):
+        """dX [Ns, H] (fp32, the dout of the last layer's backward) and the weight gradients."""
+        s = saved
+        dh, dW = P.psattn_logprob_bwd(s["h"], self.W["W"], s["tgt_ptr"], s["tgt"], s["lse"], dlogp, logit_scale=self.scale)
+        dh = dh.float()
+        xn = s["X"].float() * s["r"]
+        dhh = dh * self.W["g"].float()
+        dX = (dhh - xn * (dhh * xn).mean(-1, keepdim=True)) * s["r"]
+        return dX, {"g": (dh * xn).sum(0), "W": dW}
+
+
+def adamw(layers, head, state_bits: int = 32) -> P.AdamW:
+    """The optimizer of a stack of layers and its head: every weight in train_step's order, no decay on the norms' gains."""
+    weights = [(k, w) for part in (*layers, head) for k, w in part.W.items()]
+    return P.AdamW([w for _, w in weights], state_bits=state_bits, decay=[0.0 if k in ("g", "g1", "g2") else 1.0 for k, _ in weights])
+
+
+def train_step(layers, head, opt: P.AdamW, tree: P.Tree, X, pools, tgt_ptr, tgt, adjoint, **hyper):
+    """One training step over the shared rows: the layers and the head forward, adjoint(logp) -> dlogp (the gradient of the
+    loss by the log-probabilities), their backward, and opt.step(..., **hyper) on every weight.  pools: (K, V) per layer.
+    Returns (logp, dX, what opt.step returns)."""
+    saved, x = [], X
+    for layer, (K, V) in zip(layers, pools):
+        x, s = layer.forward(tree, x, K, V)
+        saved.append(s)
+    logp, s = head.forward(x, tgt_ptr, tgt)
+    dx, gh = head.backward(s, adjoint(logp))
+    grads = [gh[k] for k in head.W]
+    for layer, s in zip(reversed(list(layers)), reversed(saved)):
+        dx, g = layer.backward(tree, s, dx)
+        grads = [g[k] for k in layer.W] + grads
+    return logp, dx, opt.step(grads, **hyper)

@@ -9,6 +9,8 @@ Names follow the C ABI in include/psattn.h:
     Tree(...)                       psattn_tree_create / _upload / _destroy
     psattn_fwd(tree, Q, K, V)       -> (O, LSE)   (O_lo=: the bf16 rounding residual of O)
     psattn_bwd(tree, Q, K, V, O, LSE, dO) -> (dQ, dK, dV)   (O_lo=: Delta from O + O_lo)
+    psattn_logprob_fwd(X, W, tgt_ptr, tgt) -> (logp, LSE), psattn_logprob_bwd(...) -> (dX, dW)
+    AdamW(params)                   psattn_adamw_create / _upload / _step / _destroy
 """
 from __future__ import annotations
 
@@ -41,6 +43,9 @@ EXPORTED = [
     "psattn_sched_fit", "psattn_sched_group_costs", "psattn_sched_place", "psattn_sched_microbatch",
     "psattn_sched_mb_get", "psattn_sched_mb_destroy", "psattn_rope", "psattn_kv_scatter", "psattn_kv_gather",
     "psattn_split_planes", "psattn_silu_bwd",
+    "psattn_logprob_workspace_size", "psattn_logprob_fwd", "psattn_logprob_bwd",
+    "psattn_adamw_create", "psattn_adamw_destroy", "psattn_adamw_device_bytes", "psattn_adamw_upload",
+    "psattn_adamw_workspace_size", "psattn_adamw_step",
 ]
 
 KVM_EVENTS = {0: "alloc", 1: "refill", 2: "evict", 3: "free"}
@@ -103,6 +108,23 @@ class SchedMbView(ctypes.Structure):
 class PlanOpts(ctypes.Structure):
     _fields_ = [("fwd_kv_split", ctypes.c_int32), ("bwd_q_chunk", ctypes.c_int32), ("num_cus", ctypes.c_int32),
                 ("reserved", ctypes.c_int32 * 5)]
+
+
+class LogprobDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("targets", ctypes.c_int64), ("hidden", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("logit_scale", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("master", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p), ("n", ctypes.c_int64), ("decay", ctypes.c_float),
+                ("dtype", ctypes.c_int32)]
+
+
+class AdamwHyper(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("max_norm", ctypes.c_double), ("grad_scale", ctypes.c_double),
+                ("step", ctypes.c_int64), ("seed", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
 class TreeInfo(ctypes.Structure):
@@ -169,8 +191,19 @@ def lib() -> ctypes.CDLL:
         L.psattn_split_planes.argtypes = [vp, vp, ctypes.c_int64, vp]
         L.psattn_silu_bwd.argtypes = [vp, vp, vp, vp, vp, ctypes.c_int64, vp]
         L.psattn_sched_mb_destroy.restype = None
+        lpd = ctypes.POINTER(LogprobDesc)
+        L.psattn_logprob_workspace_size.argtypes = [lpd, ctypes.c_int, ctypes.POINTER(sz)]
+        L.psattn_logprob_fwd.argtypes = [lpd, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.psattn_logprob_bwd.argtypes = [lpd, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.psattn_adamw_create.argtypes = [ctypes.c_int32, ctypes.POINTER(AdamwTensor), ctypes.c_int32, ctypes.POINTER(vp)]
+        L.psattn_adamw_destroy.argtypes = [vp]
+        L.psattn_adamw_device_bytes.argtypes = [vp, ctypes.POINTER(sz)]
+        L.psattn_adamw_upload.argtypes = [vp, vp, sz, vp]
+        L.psattn_adamw_workspace_size.argtypes = [vp, ctypes.POINTER(sz)]
+        L.psattn_adamw_step.argtypes = [vp, ctypes.POINTER(vp), _i32p, ctypes.POINTER(AdamwHyper), vp, vp, vp, sz, vp]
+        L.psattn_adamw_destroy.restype = None
         for name in EXPORTED:
-            if name not in ("psattn_tree_destroy", "psattn_status_string", "psattn_last_error"):
+            if name not in ("psattn_tree_destroy", "psattn_status_string", "psattn_last_error", "psattn_adamw_destroy"):
                 getattr(L, name).restype = ctypes.c_int
         _LIB = L
     return _LIB
@@ -573,6 +606,224 @@ def psattn_silu_bwd(dM, A, B):
     return dA, dB
 
 
+def _same_device(x, *others):
+    for t, name in others:
+        if t is not None and t.device != x.device:
+            raise ValueError(f"{name} is on {t.device}, not on {x.device}")
+
+
+def _logprob_args(X, W, tgt_ptr, tgt, logit_scale):
+    import torch
+    if not isinstance(X, torch.Tensor) or not isinstance(W, torch.Tensor):
+        raise TypeError("X and W must be torch tensors")
+    if X.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("X must be bf16 or fp32")
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError(f"expected X [rows, hidden] and W [vocab, hidden], got {tuple(X.shape)} and {tuple(W.shape)}")
+    _need(X, X.shape, X.dtype, "X")
+    _need(W, (W.shape[0], X.shape[1]), X.dtype, "W")
+    _need(tgt_ptr, (X.shape[0] + 1,), torch.int32, "tgt_ptr")
+    _need(tgt, (tgt.numel(),), torch.int32, "tgt")
+    _same_device(X, (W, "W"), (tgt_ptr, "tgt_ptr"), (tgt, "tgt"))
+    return LogprobDesc(X.shape[0], tgt.numel(), X.shape[1], W.shape[0], float(logit_scale),
+                       PSATTN_BF16 if X.dtype == torch.bfloat16 else PSATTN_FP32)
+
+
+def _logprob_ws(desc, pass_, ws, X):
+    import torch
+    n = ctypes.c_size_t()
+    _check(lib().psattn_logprob_workspace_size(ctypes.byref(desc), pass_, ctypes.byref(n)))
+    if ws is None:
+        ws = torch.empty(n.value, dtype=torch.uint8, device=X.device)
+    _need(ws, (ws.numel(),), torch.uint8, "ws")
+    _same_device(X, (ws, "ws"))
+    return ws
+
+
+def psattn_logprob_workspace_size(rows: int, hidden: int, vocab: int, dtype: str = "bf16", pass_: int = 0) -> int:
+    """Workspace bytes of psattn_logprob_fwd (pass 0) or psattn_logprob_bwd (1)."""
+    n = ctypes.c_size_t()
+    desc = LogprobDesc(int(rows), 0, int(hidden), int(vocab), 1.0, PSATTN_BF16 if dtype == "bf16" else PSATTN_FP32)
+    _check(lib().psattn_logprob_workspace_size(ctypes.byref(desc), int(pass_), ctypes.byref(n)))
+    return n.value
+
+
+def psattn_logprob_fwd(X, W, tgt_ptr, tgt, logit_scale: float = 1.0, logp=None, LSE=None, ws=None):
+    """Log-probabilities of the target tokens of each row over a vocabulary, without its logits in memory;
+    returns (logp [targets], LSE [rows]), fp32.  X [rows, hidden] and W [vocab, hidden] (bf16 or fp32); row r's targets are
+    tgt[tgt_ptr[r]:tgt_ptr[r + 1]] (int32; one outside the vocabulary has logp 0)."""
+    import torch
+    desc = _logprob_args(X, W, tgt_ptr, tgt, logit_scale)
+    if logp is None:
+        logp = torch.empty(tgt.numel(), dtype=torch.float32, device=X.device)
+    if LSE is None:
+        LSE = torch.empty(X.shape[0], dtype=torch.float32, device=X.device)
+    _need(logp, (tgt.numel(),), torch.float32, "logp")
+    _need(LSE, (X.shape[0],), torch.float32, "LSE")
+    _same_device(X, (logp, "logp"), (LSE, "LSE"))
+    ws = _logprob_ws(desc, 0, ws, X)
+    with torch.cuda.device(X.device):
+        _check(lib().psattn_logprob_fwd(ctypes.byref(desc), _vp(X), _vp(W), _vp(tgt_ptr), _vp(tgt), _vp(logp), _vp(LSE), _vp(ws),
+                                        ws.numel(), ctypes.c_void_p(torch.cuda.current_stream(X.device).cuda_stream)))
+    return logp, LSE
+
+
+def psattn_logprob_bwd(X, W, tgt_ptr, tgt, LSE, dlogp, logit_scale: float = 1.0, dX=None, dW=None, need_dX: bool = True,
+                       need_dW: bool = True, ws=None):
+    """Gradients (dX, dW) of the log-probabilities for their adjoints dlogp [targets] (fp32), in the inputs' dtype; None
+    for one that is not needed.  LSE is the forward's.  Rows without a target of non-zero dlogp give 0, whatever they hold."""
+    import torch
+    desc = _logprob_args(X, W, tgt_ptr, tgt, logit_scale)
+    _need(LSE, (X.shape[0],), torch.float32, "LSE")
+    _need(dlogp, (tgt.numel(),), torch.float32, "dlogp")
+    need_dX, need_dW = need_dX or dX is not None, need_dW or dW is not None
+    if need_dX and dX is None:
+        dX = torch.empty_like(X)
+    if need_dW and dW is None:
+        dW = torch.empty_like(W)
+    for x, like, name in ((dX, X, "dX"), (dW, W, "dW")):
+        if x is not None:
+            _need(x, like.shape, X.dtype, name)
+    _same_device(X, (LSE, "LSE"), (dlogp, "dlogp"), (dX, "dX"), (dW, "dW"))
+    ws = _logprob_ws(desc, 1, ws, X)
+    with torch.cuda.device(X.device):
+        _check(lib().psattn_logprob_bwd(ctypes.byref(desc), _vp(X), _vp(W), _vp(tgt_ptr), _vp(tgt), _vp(LSE), _vp(dlogp), _vp(dX),
+                                        _vp(dW), _vp(ws), ws.numel(),
+                                        ctypes.c_void_p(torch.cuda.current_stream(X.device).cuda_stream)))
+    return dX, dW
+
+
+class AdamW:
+    """AdamW over a list of weights (psattn_adamw_*): fp32 tensors, or bf16 ones with fp32 masters, updated in place.
+
+    ``state_bits`` 32 keeps m and v in fp32.  8 keeps m and r = sqrt(v) as e4m3 codes (torch.float8_e4m3fn) with
+    one power of two per 256 elements (``m_exp``, ``r_exp``: uint8, biased by 127), rounded at random.  ``decay``
+    (one number per tensor, default 1) multiplies ``weight_decay``.  ``state`` may give the lists ``master``, ``m``, ``v``
+    (or ``m``, ``m_exp``, ``r``, ``r_exp``) to go on from; they are used as they are, not copied.  Without it masters start as
+    the weights' values and the averages as zeros.  The tensors stay where they are for the life of the object."""
+
+    def __init__(self, params, state_bits: int = 32, decay=None, state=None):
+        import torch
+        self._handle = None
+        self.params = list(params)
+        self.state_bits = int(state_bits)
+        if not self.params:
+            raise ValueError("no tensors")
+        if self.state_bits not in (8, 32):
+            raise ValueError(f"state_bits must be 8 or 32 (got {state_bits})")
+        n = len(self.params)
+        decay = [1.0] * n if decay is None else [float(d) for d in decay]
+        if len(decay) != n:
+            raise ValueError(f"{len(decay)} decay factors for {n} tensors")
+        for i, p in enumerate(self.params):
+            if not isinstance(p, torch.Tensor):
+                raise TypeError(f"params[{i}] must be a torch tensor")
+            if p.dtype not in (torch.bfloat16, torch.float32):
+                raise ValueError(f"params[{i}] must be bf16 or fp32, got {p.dtype}")
+            _need(p, p.shape, p.dtype, f"params[{i}]")
+            _same_device(self.params[0], (p, f"params[{i}]"))
+        self.device = self.params[0].device
+        given = dict(state or {})
+        new = lambda p, dtype, shape=None: torch.zeros(shape or p.shape, dtype=dtype, device=p.device)
+        blocks = lambda p: ((p.numel() + 255) // 256,)
+        f32, bf16 = torch.float32, torch.bfloat16
+        if any(p.dtype == bf16 for p in self.params):
+            self.master = list(given.pop("master", None) or [p.detach().float() if p.dtype == bf16 else None for p in self.params])
+        else:
+            self.master = list(given.pop("master", None) or [None] * n)
+        if self.state_bits == 32:
+            names = {"m": f32, "v": f32}
+        else:
+            names = {"m": torch.float8_e4m3fn, "m_exp": torch.uint8, "r": torch.float8_e4m3fn, "r_exp": torch.uint8}
+        for name, dt in names.items():
+            x = given.pop(name, None)
+            if x is None:
+                x = [new(p, dt, blocks(p) if name.endswith("_exp") else None) + (1 if name.endswith("_exp") else 0) if dt == torch.uint8
+                     else torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(dt) if dt == torch.float8_e4m3fn else new(p, dt)
+                     for p in self.params]
+            setattr(self, name, list(x))
+        if given:
+            raise ValueError(f"unknown state {sorted(given)}")
+        rec = (AdamwTensor * n)()
+        for name in ("master", *names):
+            if len(getattr(self, name)) != n:
+                raise ValueError(f"state {name}: {len(getattr(self, name))} tensors for {n} weights")
+        for i, p in enumerate(self.params):
+            for name, dt in (("master", f32), *names.items()):
+                x = getattr(self, name)[i]
+                if name == "master" and p.dtype == f32:
+                    if x is not None:
+                        raise ValueError(f"master[{i}]: fp32 weights have none")
+                    continue
+                shape = blocks(p) if name.endswith("_exp") else p.shape
+                _need(x, shape, dt, f"{name}[{i}]")
+                _same_device(p, (x, f"{name}[{i}]"))
+            ptr = lambda name: getattr(self, name)[i].data_ptr() if getattr(self, name)[i] is not None else None
+            v = "v" if self.state_bits == 32 else "r"
+            rec[i] = AdamwTensor(p.data_ptr(), ptr("master"), ptr("m"), ptr(v), ptr("m_exp") if v == "r" else None,
+                                 ptr("r_exp") if v == "r" else None, p.numel(), decay[i],
+                                 PSATTN_BF16 if p.dtype == bf16 else PSATTN_FP32)
+        L = lib()
+        h = ctypes.c_void_p()
+        _check(L.psattn_adamw_create(n, rec, self.state_bits, ctypes.byref(h)))
+        self._handle = h
+        size = ctypes.c_size_t()
+        _check(L.psattn_adamw_device_bytes(h, ctypes.byref(size)))
+        self._table = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        with torch.cuda.device(self.device):
+            _check(L.psattn_adamw_upload(h, _vp(self._table), size.value,
+                                         ctypes.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)))
+        _check(L.psattn_adamw_workspace_size(h, ctypes.byref(size)))
+        self._ws_bytes = size.value
+        self._sizes = [p.numel() for p in self.params]
+        self._pointers = ctypes.c_void_p * n
+        self._dtypes = ctypes.c_int32 * n
+
+    def __del__(self):
+        if getattr(self, "_handle", None) is not None and _LIB is not None:
+            _LIB.psattn_adamw_destroy(self._handle)
+            self._handle = None
+
+    def step(self, grads, lr: float, step: int, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
+             max_norm: float = 0.0, grad_scale: float = 1.0, seed: int = 0, dyn=None):
+        """One step on the current stream.  grads: a tensor per weight (bf16 or fp32, contiguous, of its size), or None for a
+        weight that is left as it is.  ``step`` counts from 1.  max_norm > 0 clips by the global norm (and does nothing
+        where that is not finite); the norm before clipping is then returned (fp32 [1]), else None.  ``dyn`` (int32 [4] on
+        the GPU, see :meth:`dyn`): lr, grad_scale, step and seed are read from it instead, also by replays of a captured step."""
+        import torch
+        if len(grads) != len(self.params):
+            raise ValueError(f"{len(grads)} gradients for {len(self.params)} weights")
+        f32, bf16, device = torch.float32, torch.bfloat16, self.device
+        for i, (g, n) in enumerate(zip(grads, self._sizes)):
+            if g is not None and (g.numel() != n or (g.dtype is not f32 and g.dtype is not bf16) or g.device != device or not g.is_contiguous()):
+                raise ValueError(f"grads[{i}]: expected {n} contiguous bf16 or fp32 elements on {device}, got {g.dtype} {tuple(g.shape)} on {g.device}")
+        if dyn is not None:
+            _need(dyn, (4,), torch.int32, "dyn")
+            _same_device(self.params[0], (dyn, "dyn"))
+        norm = torch.empty(1, dtype=f32, device=device) if max_norm > 0 else None
+        ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=device)
+        hyper = AdamwHyper(lr, betas[0], betas[1], eps, weight_decay, max_norm, grad_scale, step, seed & 0xffffffff, 0)
+        with torch.cuda.device(device):
+            _check(lib().psattn_adamw_step(self._handle, self._pointers(*[0 if g is None else g.data_ptr() for g in grads]),
+                                           self._dtypes(*[PSATTN_BF16 if g is not None and g.dtype is bf16 else PSATTN_FP32 for g in grads]),
+                                           ctypes.byref(hyper), _vp(dyn), _vp(norm), _vp(ws), self._ws_bytes,
+                                           ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)))
+        return norm
+
+    def dyn(self, lr: float, step: int, grad_scale: float = 1.0, seed: int = 0, out=None):
+        """The values of one step in device memory, for ``step(..., dyn=)``; out: an earlier one to be overwritten."""
+        import torch
+        host = np.zeros(4, dtype=np.int32)
+        host.view(np.float32)[:2] = lr, grad_scale
+        host[2] = step
+        host.view(np.uint32)[3] = seed & 0xffffffff
+        t = torch.from_numpy(host)
+        if out is None:
+            return t.to(self.device)
+        _need(out, (4,), torch.int32, "out")
+        return out.copy_(t)
+
+
 def psattn_profile_enable(on: bool = True) -> None:
     _check(lib().psattn_profile_enable(1 if on else 0))
 
@@ -584,7 +835,7 @@ def psattn_profile_reset() -> None:
 def psattn_profile_read() -> dict:
     """{kernel name: (launches, total ms)} since the last reset (waits for the recorded events)."""
     n = ctypes.c_int32()
-    cap = 16
+    cap = 32
     names = (ctypes.c_char_p * cap)()
     launches = (ctypes.c_int64 * cap)()
     ms = (ctypes.c_double * cap)()

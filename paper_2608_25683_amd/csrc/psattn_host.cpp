@@ -1375,6 +1375,11 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   a.pieces = (int32_t)((vr + each - 1) / each);
   a.piece_v = (int32_t)(256 * each);
   a.splits = 1;
+  if ((int64_t)(a.n / 32 + 1) * (std::max(a.v, a.h) / 128 + 1) > INT32_MAX)
+    return fail(PSATTN_E_UNSUPPORTED, "rows %d x vocab %d: more tiles than a launch holds", a.n, a.v);
+  const int64_t large = (int64_t)((a.n + 255) / 256) * ((a.v + 255) / 256);
+  a.shape = !bwd && a.n <= 32 ? LP_THIN : large >= 256 ? LP_LARGE : LP_SMALL;
+  a.part_v = a.shape == LP_LARGE ? 256 : 128;
   size_t cur = 0;
   auto take = [&](size_t bytes) {
     const size_t at = cur;
@@ -1385,7 +1390,7 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   if (copy) p.xc = take((size_t)a.planes * a.np * a.hp * 2);
   if (fp32) p.wc = take((size_t)a.planes * a.piece_v * a.hp * 2);
   if (!bwd) {
-    p.part = take((size_t)((a.v + LP_PART - 1) / LP_PART) * a.n * sizeof(LogprobStat));
+    p.part = take((size_t)((a.v + a.part_v - 1) / a.part_v) * a.n * sizeof(LogprobStat));
   } else {
     p.total = take((size_t)a.n * 4);
     p.dl = take((size_t)a.planes * a.np * a.piece_v * 2);

@@ -57,6 +57,8 @@ struct BwdArgs {
 struct LogprobStat { float top, sum; };   // max of z log2(e) and the sum of exp2(z log2(e) - max)
 struct LogprobArgs {
   int32_t n, h, v, e;        // rows, hidden, vocabulary, targets
+  int32_t shape;             // LP_THIN .. LP_LARGE
+  int32_t part_v;            // forward: entries per part, those of a tile
   int32_t planes;            // 1: bf16.  3: fp32 as three bf16 planes
   int32_t hp, np;            // h and n rounded up to 64: the padding of xc and dl holds zeros
   int32_t piece_v;           // entries per piece, a multiple of 256
@@ -73,14 +75,14 @@ struct LogprobArgs {
   float* lse_out;
   void* dX;
   void* dW;
-  LogprobStat* part;         // forward: [tiles of LP_PART vocabulary entries][n]
+  LogprobStat* part;         // forward: [parts of the vocabulary][n]
   float* total;              // backward: [n] sum of a row's live dlogp
   uint16_t* xc;              // [planes][np][hp]: X as the products take it; backward: zero in rows that have no gradient
   uint16_t* wc;              // fp32: [planes][piece_v][hp] planes of the piece
   uint16_t* dl;              // backward: [planes][np][piece_v] dz of the piece
   float* dx_acc;             // backward: [splits][n][h] sums over the pieces, where there is more than one piece or split
 };
-constexpr int LP_PART = 128;
+enum { LP_THIN, LP_SMALL, LP_LARGE };   // tiles of 128 x 32, 128 x 128, 256 x 256 (entries or hidden x rows or entries)
 
 // AdamW (psattn_adamw.hip)
 struct AdamwTensor {

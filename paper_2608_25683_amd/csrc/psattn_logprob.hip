@@ -16,60 +16,188 @@ namespace {
 
 using namespace dev;
 
-constexpr int TM = 128, TN = 128, BK = 64, LDK = BK + 8;
+constexpr int BK = 64;   // elements of the summed dimension per stage
+
+// The workgroups' shapes: WM x WN wavefronts, each with FM x FN tiles of 32 x 32.
+template <int WM_, int WN_, int FM_, int FN_>
+struct Shape2 {
+  static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, WAVES = WM * WN, THREADS = 64 * WAVES, M = 32 * WM * FM, N = 32 * WN * FN;
+  static constexpr int STAGE = (M + N) * BK * 2, LDS = 2 * STAGE;
+};
+using Large = Shape2<2, 4, 4, 2>;    // 256 x 256, one workgroup per CU
+using Small = Shape2<2, 2, 2, 2>;    // 128 x 128, two
+using Thin = Shape2<4, 1, 1, 1>;     // 128 x 32, four
 
 // An operand of a product: element (i, k) of plane q at p + q plane + i ld + k, or + k ld + i where K is the outer dimension.
-// Elements of i >= rows or k >= ks are 0.
+// Reads of i >= rows and k >= ks give some element of the operand in their place: such i are not stored, and at
+// such k the other operand holds zeros.
 struct Operand {
   const bf16_t* p;
   int64_t ld, plane;
   int rows, ks;
 };
-__constant__ const int kPairA[6] = {2, 1, 0, 1, 0, 0}, kPairB[6] = {0, 1, 2, 0, 1, 0};
 
-template <bool KOUTER>
-__device__ __forceinline__ void load_tile(bf16_t (*lds)[LDK], const Operand& o, int q, int64_t i0, int64_t k0) {
-  const bf16_t* p = o.p + q * o.plane;
-  for (int c = threadIdx.x; c < TM * BK / 8; c += 256) {
-    u32x4 x = {0, 0, 0, 0};
-    if (!KOUTER) {
-      const int i = c / (BK / 8), k = c % (BK / 8) * 8;
-      if (i0 + i < o.rows && k0 + k < o.ks) x = ld16(p + (i0 + i) * o.ld + k0 + k);
-      *(u32x4*)&lds[i][k] = x;
-    } else {
-      const int k = c / (TM / 8), i = c % (TM / 8) * 8;
-      if (i0 + i < o.rows && k0 + k < o.ks) x = ld16(p + (k0 + k) * o.ld + i0 + i);
+// One operand's share of a stage, copied to LDS without registers.  A copy instruction moves 1 KB.
+// K inner: rows of 64 elements (128 bytes, 8 chunks of 16), chunk c of row i at position c ^ ((i >> 1) & 7): 16 rows read at one
+// column hit distinct banks.  K outer: rows of I elements, chunk c of row k at position c ^ ((k & 3) << 2): the transposing reads
+// take 4 rows x 4 chunks, distinct banks again.
+template <int I, int WAVES, bool KOUTER>
+struct Loader {
+  static constexpr int COUNT = I * BK * 2 / 1024 / WAVES;
+  static_assert(COUNT * 1024 * WAVES == I * BK * 2, "whole instructions");
+  const bf16_t* p;       // element (i0, 0) of the plane
+  int64_t step;          // bytes from one stage to the next
+  uint32_t off[COUNT];   // of each instruction's lane, from the stage's first element
+  __device__ __forceinline__ Loader(const Operand& o, int64_t i0) : p(o.p + (KOUTER ? i0 : i0 * o.ld)), step(KOUTER ? BK * o.ld * 2 : BK * 2) {}
+  // offsets for stages of which klim elements (1 .. 64) lie inside the operand
+  __device__ __forceinline__ void aim(const Operand& o, int64_t i0, int klim, int wave, int lane) {
+    const int ilim = (int)min((int64_t)I, o.rows - i0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) lds[i + e][k] = (bf16_t)(x[e / 2] >> (16 * (e & 1)));
-    }
-  }
-}
-
-// acc[f] = A rows i0 + 32 f .. (down the 32 x 32 tile) x B rows j0 + 32 wave .. (across) over k < ks
-template <bool KA, bool KB>
-__device__ __forceinline__ void product(f32x16 (&acc)[4], const Operand& A, const Operand& B, int planes, int64_t i0, int64_t j0, int ks) {
-  __shared__ __attribute__((aligned(16))) bf16_t sa[TM][LDK], sb[TN][LDK];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int f = 0; f < 4; ++f)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[f][e] = 0.f;
-  for (int q = planes == 3 ? 0 : 5; q < 6; ++q)
-    for (int k0 = 0; k0 < ks; k0 += BK) {
-      __syncthreads();
-      load_tile<KA>(sa, A, kPairA[q], i0, k0);
-      load_tile<KB>(sb, B, kPairB[q], j0, k0);
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < BK; k += 16) {
-        const bf16x8 b = as_bf(ld16(&sb[32 * wave + (lane & 31)][k + 8 * (lane >> 5)]));
-#pragma unroll
-        for (int f = 0; f < 4; ++f) acc[f] = mfma(as_bf(ld16(&sa[32 * f + (lane & 31)][k + 8 * (lane >> 5)])), b, acc[f]);
+    for (int j = 0; j < COUNT; ++j) {
+      const int u = wave * COUNT + j;
+      if (KOUTER) {
+        const int per = I / 8, k = u * (512 / I) + lane / per;
+        int c = (lane % per) ^ ((k & 3) << 2);
+        if (8 * c >= ilim) c = 0;
+        off[j] = (uint32_t)(min(k, klim - 1) * (int)o.ld * 2 + 16 * c);
+      } else {
+        const int i = u * 8 + (lane >> 3);
+        int c = (lane & 7) ^ ((i >> 1) & 7);
+        if (8 * c >= klim) c = 0;
+        off[j] = (uint32_t)(min(i, ilim - 1) * (int)o.ld * 2 + 16 * c);
       }
     }
+  }
+  __device__ __forceinline__ void issue(const char* base, uint32_t lds, int wave) const {
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j) copy16_to_lds_off(base, off[j], lds + (wave * COUNT + j) * 1024);
+  }
+};
+
+// A wavefront's reads of an operand's tile: FRAGS tiles of 32 rows from row i on.
+template <int I, int FRAGS, bool KOUTER>
+struct Reader {
+  uint32_t at[KOUTER ? FRAGS : 4];
+  __device__ __forceinline__ Reader(int i, int lane) {
+    if (KOUTER) {
+      const int l = lane & 15, k = 8 * (lane >> 5) + (l >> 2);
+#pragma unroll
+      for (int f = 0; f < FRAGS; ++f) {
+        const int c = (i + 32 * f) / 8 + 2 * ((lane >> 4) & 1) + ((l & 3) >> 1);
+        at[f] = k * I * 2 + ((c ^ ((k & 3) << 2)) << 4) + (l & 1) * 8;
+      }
+    } else {
+      const int r = i + (lane & 31);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) at[kk] = r * BK * 2 + (((2 * kk + (lane >> 5)) ^ ((r >> 1) & 7)) << 4);
+    }
+  }
+  template <int KK>
+  __device__ __forceinline__ void read(bf16x8 (&x)[FRAGS], const uint8_t* tile) const {
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f) {
+      if constexpr (KOUTER) {
+        const uint8_t* p = tile + at[f] + KK * 16 * I * 2;
+        x[f] = as_bf(lds_tr(p), lds_tr(p + 4 * I * 2));
+      } else {
+        x[f] = as_bf(ld16(tile + at[KK] + f * 32 * BK * 2));
+      }
+    }
+  }
+};
+
+// acc = A rows i0 .. i0 + M - 1 (down the tiles) x B rows j0 .. j0 + N - 1 (across) over ks elements (all there are, padded to
+// a multiple of 64).  Two stages in LDS: while one is multiplied, the next is copied.  The barrier between two stages
+// stands before the last quarter of a stage's products, whose operands are in registers by then, so that they cover
+// the first reads of the next stage.
+template <class S, bool KA, bool KB>
+__device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Operand& A, const Operand& B, int planes, int64_t i0, int64_t j0,
+                                        int ks, uint8_t* lds) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+  for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+    for (int g = 0; g < S::FN; ++g)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[f][g][e] = 0.f;
+  const int nk = (ks + BK - 1) / BK, steps = planes == 3 ? 6 * nk : nk;
+  if (steps == 0) return;
+  Loader<S::M, S::WAVES, KA> la(A, i0);
+  Loader<S::N, S::WAVES, KB> lb(B, j0);
+  const Reader<S::M, S::FM, KA> ra(wave / S::WN * S::FM * 32, lane);
+  const Reader<S::N, S::FN, KB> rb(wave % S::WN * S::FN * 32, lane);
+  const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(lds));
+  const bool ragged = min(A.ks, B.ks) < nk * BK;
+  int pair = planes == 3 ? 0 : 5, kt = 0;
+  la.aim(A, i0, BK, wave, lane);
+  lb.aim(B, j0, BK, wave, lane);
+  auto issue = [&](int stage) {
+    if (ragged && (kt == nk - 1 || kt == 0)) {   // (the last stage of a plane, and the first behind it)
+      la.aim(A, i0, min(BK, A.ks - kt * BK), wave, lane);
+      lb.aim(B, j0, min(BK, B.ks - kt * BK), wave, lane);
+    }
+    // the planes of A and B by pair: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
+    const int pa = pair == 0 ? 2 : pair == 1 || pair == 3 ? 1 : 0, pb = pair == 2 ? 2 : pair == 1 || pair == 4 ? 1 : 0;
+    la.issue((const char*)(la.p + pa * A.plane) + kt * la.step, at + stage * S::STAGE, wave);
+    lb.issue((const char*)(lb.p + pb * B.plane) + kt * lb.step, at + stage * S::STAGE + S::M * BK * 2, wave);
+    if (++kt == nk) {
+      kt = 0;
+      ++pair;
+    }
+  };
+  bf16x8 fa[2][S::FM], fb[2][S::FN];
+  issue(0);
+  wait_vmem<0>();
+  barrier_only();
+  if (steps > 1) issue(1);
+  ra.template read<0>(fa[0], lds);
+  rb.template read<0>(fb[0], lds + S::M * BK * 2);
+  for (int s = 0; s < steps; ++s) {
+    const uint8_t* tile = lds + (s & 1) * S::STAGE;
+    const uint8_t* next = lds + (~s & 1) * S::STAGE;
+    static_for<4>([&](auto q) {
+      constexpr int KK = decltype(q)::value;
+      if constexpr (KK < 3) {
+        ra.template read<(KK + 1) & 3>(fa[(KK + 1) & 1], tile);
+        rb.template read<(KK + 1) & 3>(fb[(KK + 1) & 1], tile + S::M * BK * 2);
+      } else if (s + 1 < steps) {
+        wait_lds<0>();
+        wait_vmem<0>();
+        barrier_only();
+        if (s + 2 < steps) issue(s & 1);
+        ra.template read<0>(fa[0], next);
+        rb.template read<0>(fb[0], next + S::M * BK * 2);
+      }
+#pragma unroll
+      for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+        for (int g = 0; g < S::FN; ++g) acc[f][g] = mfma(fa[KK & 1][f], fb[KK & 1][g], acc[f][g]);
+    });
+  }
+  wait_lds<0>();
+  barrier_only();   // (the LDS is the caller's again)
 }
 // the row down the 32 x 32 tile of element e of a lane
 __device__ __forceinline__ int down(int e, int lane) { return 8 * (e / 4) + 4 * (lane >> 5) + e % 4; }
+// The four dwords of bf16 that lanes l and l + 32 hold of tile rows 16 h .. 16 h + 15, as 8 consecutive rows each: lanes below
+// 32 get rows 16 h .., the others 16 h + 8 ..
+__device__ __forceinline__ u32x4 rows8(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
+  const auto x = __builtin_amdgcn_permlane32_swap(a0, b0, false, false);
+  const auto y = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+  return u32x4{(uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]};
+}
+
+// Which tile a workgroup takes.  Workgroups go to the 8 XCDs in turn; those of one XCD take consecutive tiles, in bands of
+// `band` tiles down by all tiles across, so that the 32 that run on it at a time share rows of both operands in its L2.
+struct Tile { int down, across; };
+__device__ __forceinline__ Tile tile_of(int downs, int acrosses, int band) {
+  const int total = downs * acrosses, per = total / 8, rest = total % 8;
+  const int x = blockIdx.x % 8, at = blockIdx.x / 8;
+  const int t = x * per + min(x, rest) + at;
+  const int b = t / (band * acrosses), first = b * band, high = min(band, downs - first), in = t - first * acrosses;
+  // (divisions leave uniform values in vector registers)
+  return {__builtin_amdgcn_readfirstlane(first + in % high), __builtin_amdgcn_readfirstlane(in / high)};
+}
 
 __device__ __forceinline__ Operand x_operand(const LogprobArgs& a) {
   if (a.xc) return {a.xc, a.hp, (int64_t)a.np * a.hp, a.np, a.hp};
@@ -81,6 +209,13 @@ __device__ __forceinline__ Operand w_operand(const LogprobArgs& a, int piece) {
   return {(const bf16_t*)a.W + (int64_t)v0 * a.h, a.h, 0, rows, a.h};
 }
 __device__ __forceinline__ Operand swapped(const Operand& o) { return {o.p, o.ld, o.plane, o.ks, o.rows}; }
+
+// the statistics of two sets of logits together
+__device__ __forceinline__ LogprobStat join(const LogprobStat& p, const LogprobStat& q) {
+  const float top = fmaxf(p.top, q.top), ref = top == kNegInf ? 0.f : top;
+  // (fmaxf leaves a NaN out: it comes through the sums)
+  return {top, p.sum * fast_exp2(p.top - ref) + q.sum * fast_exp2(q.top - ref)};
+}
 
 // bounds of a row's targets, whatever tgt_ptr holds
 __device__ __forceinline__ void targets_of(const LogprobArgs& a, int r, int& e0, int& e1) {
@@ -138,140 +273,244 @@ __global__ __launch_bounds__(256) void wplanes_kernel(LogprobArgs a, int piece) 
   }
 }
 
-// ---- a tile of logits: 128 entries of the piece down, 128 rows across
-template <bool BACKWARD>
-__global__ __launch_bounds__(256) void logits_kernel(LogprobArgs a, int piece) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i0 = (int64_t)blockIdx.x * TM, j0 = (int64_t)blockIdx.y * TN;
-  f32x16 acc[4];
+// ---- a tile of logits: M entries of the piece down, N rows across
+template <class S, bool BACKWARD>
+__global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tile tile = tile_of(downs, acrosses, 4);
+  const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
+  const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;   // the wavefront's first entry and row of the tile
+  f32x16 acc[S::FM][S::FN];
   const Operand W = w_operand(a, piece);
-  product<false, false>(acc, W, x_operand(a), a.planes, i0, j0, a.hp);
-  const int64_t r = j0 + 32 * wave + (lane & 31);
+  product<S, false, false>(acc, W, x_operand(a), a.planes, i0, j0, a.hp, lds);
   const float c = a.scale * kLog2e;
-  if (!BACKWARD) {
-    float top = kNegInf, sum = 0.f;
+  if constexpr (!BACKWARD) {
+    LogprobStat* part = (LogprobStat*)lds;                 // [WM][N]
 #pragma unroll
-    for (int f = 0; f < 4; ++f)
+    for (int g = 0; g < S::FN; ++g) {
+      float top = kNegInf, sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const bool in = i0 + 32 * f + down(e, lane) < W.rows;
-        acc[f][e] = in ? acc[f][e] * c : kNegInf;
-        top = fmaxf(top, acc[f][e]);
-      }
-    top = pair_max(top);
-    const float ref = top == kNegInf ? 0.f : top;
+      for (int f = 0; f < S::FM; ++f)
 #pragma unroll
-    for (int f = 0; f < 4; ++f)
+        for (int e = 0; e < 16; ++e) {
+          const bool in = iw + 32 * f + down(e, lane) < W.rows;
+          acc[f][g][e] = in ? acc[f][g][e] * c : kNegInf;
+          top = fmaxf(top, acc[f][g][e]);
+        }
+      top = pair_max(top);
+      const float ref = top == kNegInf ? 0.f : top;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sum += fast_exp2(acc[f][e] - ref);
-    sum = pair_sum(sum);
-    if (r < a.n && lane < 32 && i0 < W.rows) a.part[((int64_t)piece * (a.piece_v / LP_PART) + blockIdx.x) * a.n + r] = {top, sum};
+      for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum += fast_exp2(acc[f][g][e] - ref);
+      sum = pair_sum(sum);
+      if (lane < 32) part[wave / S::WN * S::N + jw + 32 * g + lane] = {top, sum};
+    }
+    __syncthreads();
+    for (int j = threadIdx.x; j < S::N; j += S::THREADS) {
+      LogprobStat p = part[j];
+#pragma unroll
+      for (int w = 1; w < S::WM; ++w) p = join(p, part[w * S::N + j]);
+      if (j0 + j < a.n) a.part[((int64_t)piece * a.piece_v / S::M + tile.down) * a.n + j0 + j] = p;
+    }
     return;
-  }
-  if (r >= a.np) return;
-  const bool in_row = r < a.n;
-  const float total = in_row ? a.total[r] : 0.f, lse2 = in_row ? a.lse[r] * kLog2e : 0.f;
-  int e0 = 0, e1 = 0;
-  if (in_row) targets_of(a, (int)r, e0, e1);
+  } else {
+    const int v0 = piece * a.piece_v;
 #pragma unroll
-  for (int f = 0; f < 4; ++f)
+    for (int g = 0; g < S::FN; ++g) {
+      const int64_t r = j0 + jw + 32 * g + (lane & 31);
+      const bool in_row = r < a.n;
+      const float total = in_row ? a.total[r] : 0.f, lse2 = in_row ? a.lse[r] * kLog2e : 0.f;
+      int e0 = 0, e1 = 0;
+      if (in_row) targets_of(a, (int)r, e0, e1);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t i = i0 + 32 * f + down(e, lane);
-      float d = i < W.rows && total != 0.f ? -total * fast_exp2(acc[f][e] * c - lse2) : 0.f;
-      for (int t = e0; t < e1; ++t)
-        if (a.tgt[t] == piece * a.piece_v + i && i < W.rows) d += a.dlogp[t];
-      d *= a.scale;
-      if (i >= a.piece_v) continue;
-      const int64_t at = r * a.piece_v + i, plane = (int64_t)a.np * a.piece_v;
-      if (a.planes == 1) {
-        a.dl[at] = (bf16_t)pack2(d, 0.f);
-      } else {
-        put_plane1(d, a.dl, plane, at);
+      for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[f][g][e] = total != 0.f ? -total * fast_exp2(acc[f][g][e] * c - lse2) : 0.f;
+      // the targets among the wavefront's entries: few, so each is looked for in the registers
+      for (int t = e0; __any(t < e1); ++t) {
+        int at = -1;
+        float d = 0.f;
+        if (t < e1) {
+          at = a.tgt[t];
+          at = at < 0 || at >= a.v ? -1 : at - v0 - iw;
+          d = a.dlogp[t];
+        }
+        if (!__any(at >= 0 && at < 32 * S::FM)) continue;
+#pragma unroll
+        for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (at == 32 * f + down(e, lane)) acc[f][g][e] += d;
       }
+      if (r >= a.np) continue;
+      const int64_t plane = (int64_t)a.np * a.piece_v;
+#pragma unroll
+      for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = iw + 32 * f + down(8 * h + e, lane) < W.rows ? acc[f][g][8 * h + e] * a.scale : 0.f;
+          const int i = iw + 32 * f + 16 * h + 8 * (lane >> 5);
+          if (a.planes == 1) {
+            const u32x4 y = rows8(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
+            if (i < a.piece_v) *(u32x4*)(a.dl + r * a.piece_v + i) = y;
+          } else {
+            uint32_t p[3][8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) split3(x[e], p[0][e], p[1][e], p[2][e]);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) {
+              const u32x4 y = rows8(p[q][0] | p[q][1] << 16, p[q][2] | p[q][3] << 16, p[q][4] | p[q][5] << 16, p[q][6] | p[q][7] << 16);
+              if (i < a.piece_v) *(u32x4*)(a.dl + q * plane + r * a.piece_v + i) = y;
+            }
+          }
+        }
     }
+  }
 }
 
-// ---- LSE and logp from the tiles' parts: a wavefront per row
+// ---- LSE and logp from the tiles' parts: 16 rows per workgroup, 16 threads for each row's parts, then a wavefront per target
 template <bool FP32>
-__global__ __launch_bounds__(64) void finish_kernel(LogprobArgs a) {
-  const int r = blockIdx.x, lane = threadIdx.x;
-  const int parts = (a.v + LP_PART - 1) / LP_PART;
-  float top = kNegInf, sum = 0.f;
-  for (int t = lane; t < parts; t += 64) top = fmaxf(top, a.part[(int64_t)t * a.n + r].top);
-  for (int w = 32; w >= 1; w >>= 1) top = fmaxf(top, __shfl_xor(top, w));
-  const float ref = top == kNegInf ? 0.f : top;
-  for (int t = lane; t < parts; t += 64) {
-    const LogprobStat p = a.part[(int64_t)t * a.n + r];
-    sum += p.sum * fast_exp2(p.top - ref);
-  }
-  for (int w = 32; w >= 1; w >>= 1) sum += __shfl_xor(sum, w);
-  const float lse = (ref + log2f(sum)) * (1.f / kLog2e);
-  if (lane == 0) a.lse_out[r] = lse;
-  int e0, e1;
-  targets_of(a, r, e0, e1);
-  const void* x = elem_ptr<!FP32>(a.X, (size_t)r * a.h);
-  for (int e = e0; e < e1; ++e) {
-    const int t = a.tgt[e];
-    float z = 0.f;
-    if (t >= 0 && t < a.v) {
-      for (int c = lane; c < a.h; c += 64) z = fmaf(elem<!FP32>(x, c), elem<!FP32>(elem_ptr<!FP32>(a.W, (size_t)t * a.h), c), z);
-      for (int w = 32; w >= 1; w >>= 1) z += __shfl_xor(z, w);
-      z = z * a.scale - lse;
+__global__ __launch_bounds__(256) void finish_kernel(LogprobArgs a) {
+  __shared__ LogprobStat s_part[16][17];
+  __shared__ float s_lse[16];
+  const int r0 = blockIdx.x * 16, lane = threadIdx.x & 63;
+  {
+    const int i = threadIdx.x & 15, r = r0 + i, slice = threadIdx.x >> 4;
+    const int parts = (a.v + a.part_v - 1) / a.part_v;
+    LogprobStat p = {kNegInf, 0.f};
+    if (r < a.n) {
+#pragma unroll 8
+      for (int t = slice; t < parts; t += 16) p = join(p, a.part[(int64_t)t * a.n + r]);
     }
-    if (lane == 0) a.logp[e] = z;
+    s_part[i][slice] = p;
+  }
+  __syncthreads();
+  if (threadIdx.x < 16 && r0 + (int)threadIdx.x < a.n) {
+    LogprobStat p = s_part[threadIdx.x][0];
+    for (int k = 1; k < 16; ++k) p = join(p, s_part[threadIdx.x][k]);
+    const float lse = ((p.top == kNegInf ? 0.f : p.top) + log2f(p.sum)) * (1.f / kLog2e);
+    s_lse[threadIdx.x] = lse;
+    a.lse_out[r0 + threadIdx.x] = lse;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x >> 6; i < 16 && r0 + i < a.n; i += 4) {
+    const int r = r0 + i;
+    int e0, e1;
+    targets_of(a, r, e0, e1);
+    for (int e = e0; e < e1; ++e) {
+      const int t = a.tgt[e];
+      float z = 0.f;
+      if (t >= 0 && t < a.v) {
+        constexpr int V = FP32 ? 4 : 8;   // elements in 16 bytes
+        const uint8_t* x = (const uint8_t*)elem_ptr<!FP32>(a.X, (size_t)r * a.h);
+        const uint8_t* w = (const uint8_t*)elem_ptr<!FP32>(a.W, (size_t)t * a.h);
+#pragma unroll 4
+        for (int c = lane * V; c < a.h; c += 64 * V) {
+          const u32x4 p = ld16(x + c * (16 / V)), q = ld16(w + c * (16 / V));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (FP32) {
+              z = fmaf(__uint_as_float(p[k]), __uint_as_float(q[k]), z);
+            } else {
+              z = fmaf(bf2f(p[k] & 0xffffu), bf2f(q[k] & 0xffffu), z);
+              z = fmaf(__uint_as_float(p[k] & 0xffff0000u), __uint_as_float(q[k] & 0xffff0000u), z);
+            }
+          }
+        }
+#pragma unroll
+        for (int w2 = 32; w2 >= 1; w2 >>= 1) z += __shfl_xor(z, w2);
+        z = z * a.scale - s_lse[i];
+      }
+      if (lane == 0) a.logp[e] = z;
+    }
   }
 }
 
-// one element of a result of the inputs' type
-__device__ __forceinline__ void put(void* p, int64_t i, float x, bool fp32) {
-  if (fp32) ((float*)p)[i] = x;
-  else ((bf16_t*)p)[i] = (bf16_t)pack2(x, 0.f);
+// 8 elements x of a row that the lane holds after rows8's exchange (16 rows of the tile, 8 values of this lane) to p + at in
+// the inputs' type
+__device__ __forceinline__ void put_rows(void* p, int64_t row, int i, int limit, const f32x16& x, int h, bool fp32, int lane) {
+  const int b = 8 * h;
+  if (fp32) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int at = i + 16 * h + 8 * q + 4 * (lane >> 5);
+      if (at < limit) *(f32x4*)((float*)p + row + at) = f32x4{x[b + 4 * q], x[b + 4 * q + 1], x[b + 4 * q + 2], x[b + 4 * q + 3]};
+    }
+  } else {
+    const u32x4 y = rows8(pack2(x[b], x[b + 1]), pack2(x[b + 2], x[b + 3]), pack2(x[b + 4], x[b + 5]), pack2(x[b + 6], x[b + 7]));
+    const int at = i + 16 * h + 8 * (lane >> 5);
+    if (at < limit) *(u32x4*)((bf16_t*)p + row + at) = y;
+  }
 }
 
-// dX: 128 of the hidden dimension down, 128 rows across
-__global__ __launch_bounds__(256) void dx_kernel(LogprobArgs a, int piece) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i0 = (int64_t)blockIdx.x * TM, j0 = (int64_t)blockIdx.y * TN;
-  f32x16 acc[4];
+// dX: M of the hidden dimension down, N rows across
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tile tile = tile_of(downs, acrosses, 4);
+  const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
+  const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
+  f32x16 acc[S::FM][S::FN];
   const Operand W = swapped(w_operand(a, piece));
   const Operand D = {a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.np, a.piece_v};
-  product<true, false>(acc, W, D, a.planes, i0, j0, W.ks);
-  const int64_t r = j0 + 32 * wave + (lane & 31);
-  if (r >= a.n) return;
+  product<S, true, false>(acc, W, D, a.planes, i0, j0, W.ks, lds);
 #pragma unroll
-  for (int f = 0; f < 4; ++f)
+  for (int g = 0; g < S::FN; ++g) {
+    const int64_t r = j0 + jw + 32 * g + (lane & 31);
+    const bool in = r < a.n;
+    const int limit = in ? a.h : 0;
+    const int64_t row = r * a.h;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t i = i0 + 32 * f + down(e, lane);
-      if (i >= a.h) continue;
-      float x = acc[f][e];
-      if (piece) x += a.dx_acc[r * a.h + i];
-      if (piece < a.pieces - 1) a.dx_acc[r * a.h + i] = x;
-      else put(a.dX, r * a.h + i, x, a.planes == 3);
+    for (int f = 0; f < S::FM; ++f) {
+      const int i = iw + 32 * f;
+      if (piece) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int at = i + 8 * q + 4 * (lane >> 5);
+          if (at < limit) {
+            const f32x4 y = *(const f32x4*)(a.dx_acc + row + at);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[f][g][4 * q + k] += y[k];
+          }
+        }
+      }
+      const bool last = piece == a.pieces - 1;
+      put_rows(last ? a.dX : (void*)a.dx_acc, row, i, limit, acc[f][g], 0, !last || a.planes == 3, lane);
+      put_rows(last ? a.dX : (void*)a.dx_acc, row, i, limit, acc[f][g], 1, !last || a.planes == 3, lane);
     }
+  }
 }
 
-// dW: 128 of the hidden dimension down, 128 entries across
-__global__ __launch_bounds__(256) void dw_kernel(LogprobArgs a, int piece) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i0 = (int64_t)blockIdx.x * TM, j0 = (int64_t)blockIdx.y * TN;
-  f32x16 acc[4];
+// dW: M of the hidden dimension down, N entries across
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tile tile = tile_of(downs, acrosses, 4);
+  const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
+  const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
+  f32x16 acc[S::FM][S::FN];
   const Operand X = {a.xc, a.hp, (int64_t)a.np * a.hp, a.hp, a.np};
   const Operand D = {a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, a.np};
-  product<true, true>(acc, X, D, a.planes, i0, j0, a.np);
-  const int64_t v = j0 + 32 * wave + (lane & 31), at = (int64_t)piece * a.piece_v + v;
-  if (v >= a.piece_v || at >= a.v) return;
+  product<S, true, true>(acc, X, D, a.planes, i0, j0, a.np, lds);
 #pragma unroll
-  for (int f = 0; f < 4; ++f)
+  for (int g = 0; g < S::FN; ++g) {
+    const int64_t v = j0 + jw + 32 * g + (lane & 31), at = (int64_t)piece * a.piece_v + v;
+    const int limit = v < a.piece_v && at < a.v ? a.h : 0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t i = i0 + 32 * f + down(e, lane);
-      if (i < a.h) put(a.dW, at * a.h + i, acc[f][e], a.planes == 3);
+    for (int f = 0; f < S::FM; ++f) {
+      put_rows(a.dW, at * a.h, iw + 32 * f, limit, acc[f][g], 0, a.planes == 3, lane);
+      put_rows(a.dW, at * a.h, iw + 32 * f, limit, acc[f][g], 1, a.planes == 3, lane);
     }
+  }
 }
 
-unsigned tiles(int64_t n) { return (unsigned)((n + 127) / 128); }
+int tiles(int64_t n, int tile) { return (int)((n + tile - 1) / tile); }
 int piece_rows(const LogprobArgs& a, int piece) { return std::min(a.piece_v, a.v - piece * a.piece_v); }
 
 }  // namespace
@@ -285,24 +524,42 @@ hipError_t launch_logprob_wplanes(const LogprobArgs& a, int piece, hipStream_t s
   hipLaunchKernelGGL(wplanes_kernel, dim3((unsigned)a.piece_v), dim3(256), 0, st, a, piece);
   return hipGetLastError();
 }
+#define PSATTN_LP_LAUNCH(KERNEL, S, DOWN, ACROSS)                                                                          \
+  do {                                                                                                                   \
+    const int d = tiles(DOWN, S::M), c = tiles(ACROSS, S::N);                                                              \
+    hipLaunchKernelGGL(KERNEL, dim3((unsigned)((int64_t)d * c)), dim3(S::THREADS), 0, st, a, piece, d, c);                  \
+  } while (0)
+
 hipError_t launch_logprob_logits(const LogprobArgs& a, int piece, bool backward, hipStream_t st) {
-  const dim3 grid(tiles(backward ? a.piece_v : piece_rows(a, piece)), tiles(backward ? a.np : a.n));
-  if (backward) hipLaunchKernelGGL(logits_kernel<true>, grid, dim3(256), 0, st, a, piece);
-  else hipLaunchKernelGGL(logits_kernel<false>, grid, dim3(256), 0, st, a, piece);
+  const int rows = piece_rows(a, piece);
+  if (backward) {
+    if (a.shape == LP_LARGE) PSATTN_LP_LAUNCH((logits_kernel<Large, true>), Large, rows, a.np);
+    else PSATTN_LP_LAUNCH((logits_kernel<Small, true>), Small, rows, a.np);
+  } else if (a.shape == LP_LARGE) {
+    PSATTN_LP_LAUNCH((logits_kernel<Large, false>), Large, rows, a.n);
+  } else if (a.shape == LP_SMALL) {
+    PSATTN_LP_LAUNCH((logits_kernel<Small, false>), Small, rows, a.n);
+  } else {
+    PSATTN_LP_LAUNCH((logits_kernel<Thin, false>), Thin, rows, a.n);
+  }
   return hipGetLastError();
 }
 hipError_t launch_logprob_finish(const LogprobArgs& a, hipStream_t st) {
-  if (a.planes == 3) hipLaunchKernelGGL(finish_kernel<true>, dim3((unsigned)a.n), dim3(64), 0, st, a);
-  else hipLaunchKernelGGL(finish_kernel<false>, dim3((unsigned)a.n), dim3(64), 0, st, a);
+  const dim3 grid((unsigned)tiles(a.n, 16));
+  if (a.planes == 3) hipLaunchKernelGGL(finish_kernel<true>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(finish_kernel<false>, grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_logprob_dx(const LogprobArgs& a, int piece, hipStream_t st) {
-  hipLaunchKernelGGL(dx_kernel, dim3(tiles(a.h), tiles(a.n)), dim3(256), 0, st, a, piece);
+  if (a.shape == LP_LARGE) PSATTN_LP_LAUNCH(dx_kernel<Large>, Large, a.h, a.n);
+  else PSATTN_LP_LAUNCH(dx_kernel<Small>, Small, a.h, a.n);
   return hipGetLastError();
 }
 hipError_t launch_logprob_dx_sum(const LogprobArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_logprob_dw(const LogprobArgs& a, int piece, hipStream_t st) {
-  hipLaunchKernelGGL(dw_kernel, dim3(tiles(a.h), tiles(piece_rows(a, piece))), dim3(256), 0, st, a, piece);
+  const int rows = piece_rows(a, piece);
+  if (a.shape == LP_LARGE) PSATTN_LP_LAUNCH(dw_kernel<Large>, Large, a.h, rows);
+  else PSATTN_LP_LAUNCH(dw_kernel<Small>, Small, a.h, rows);
   return hipGetLastError();
 }
 

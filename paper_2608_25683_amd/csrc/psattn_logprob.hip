@@ -16,17 +16,16 @@ namespace {
 
 using namespace dev;
 
-constexpr int BK = 64;   // elements of the summed dimension per stage
-
-// The workgroups' shapes: WM x WN wavefronts, each with FM x FN tiles of 32 x 32.
-template <int WM_, int WN_, int FM_, int FN_>
+// The workgroups' shapes: WM x WN wavefronts, each with FM x FN tiles of 32 x 32; stages of BK elements of the summed dimension,
+// RING of them in LDS.
+template <int WM_, int WN_, int FM_, int FN_, int BK_, int RING_>
 struct Shape2 {
   static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, WAVES = WM * WN, THREADS = 64 * WAVES, M = 32 * WM * FM, N = 32 * WN * FN;
-  static constexpr int STAGE = (M + N) * BK * 2, LDS = 2 * STAGE;
+  static constexpr int BK = BK_, RING = RING_, STAGE = (M + N) * BK * 2, LDS = RING * STAGE;
 };
-using Large = Shape2<2, 4, 4, 2>;    // 256 x 256, one workgroup per CU
-using Small = Shape2<2, 2, 2, 2>;    // 128 x 128, two
-using Thin = Shape2<4, 1, 1, 1>;     // 128 x 32, four
+using Large = Shape2<2, 4, 4, 2, 64, 2>;    // 256 x 256, one workgroup per CU
+using Small = Shape2<2, 2, 2, 2, 64, 2>;    // 128 x 128, two
+using Thin = Shape2<4, 1, 1, 1, 64, 2>;     // 128 x 32, four
 
 // An operand of a product: element (i, k) of plane q at p + q plane + i ld + k, or + k ld + i where K is the outer dimension.
 // Reads of i >= rows and k >= ks give some element of the operand in their place: such i are not stored, and at
@@ -37,47 +36,59 @@ struct Operand {
   int rows, ks;
 };
 
+// a pointer that is the same in every lane, in scalar registers
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t u = (uint64_t)(uintptr_t)p;
+  return (const char*)(uintptr_t)((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(u >> 32)) << 32 |
+                                  (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)u));
+}
+
 // One operand's share of a stage, copied to LDS without registers.  A copy instruction moves 1 KB.
-// K inner: rows of 64 elements (128 bytes, 8 chunks of 16), chunk c of row i at position c ^ ((i >> 1) & 7): 16 rows read at one
-// column hit distinct banks.  K outer: rows of I elements, chunk c of row k at position c ^ ((k & 3) << 2): the transposing reads
+// K inner: rows of BK elements (BK / 8 chunks of 16 bytes), chunk c of row i at position c ^ swz(i): 16 rows read at one column
+// hit distinct banks.  K outer: rows of I elements, chunk c of row k at position c ^ ((k & 3) << 2): the transposing reads
 // take 4 rows x 4 chunks, distinct banks again.
-template <int I, int WAVES, bool KOUTER>
+template <int BK>
+__device__ __forceinline__ int kswz(int i) { return BK == 64 ? (i >> 1) & 7 : (i >> 2) & 3; }
+template <int I, int BK, int WAVES, bool KOUTER>
 struct Loader {
   static constexpr int COUNT = I * BK * 2 / 1024 / WAVES;
   static_assert(COUNT * 1024 * WAVES == I * BK * 2, "whole instructions");
-  const bf16_t* p;       // element (i0, 0) of the plane
+  const bf16_t* p;       // element (i0, 0) of the first plane
   int64_t step;          // bytes from one stage to the next
   uint32_t off[COUNT];   // of each instruction's lane, from the stage's first element
   __device__ __forceinline__ Loader(const Operand& o, int64_t i0) : p(o.p + (KOUTER ? i0 : i0 * o.ld)), step(KOUTER ? BK * o.ld * 2 : BK * 2) {}
-  // offsets for stages of which klim elements (1 .. 64) lie inside the operand
+  // offsets for stages of which klim elements (1 .. BK) lie inside the operand
   __device__ __forceinline__ void aim(const Operand& o, int64_t i0, int klim, int wave, int lane) {
     const int ilim = (int)min((int64_t)I, o.rows - i0);
 #pragma unroll
     for (int j = 0; j < COUNT; ++j) {
       const int u = wave * COUNT + j;
       if (KOUTER) {
-        const int per = I / 8, k = u * (512 / I) + lane / per;
+        constexpr int per = I / 8;
+        const int k = u * (64 / per) + lane / per;
         int c = (lane % per) ^ ((k & 3) << 2);
         if (8 * c >= ilim) c = 0;
         off[j] = (uint32_t)(min(k, klim - 1) * (int)o.ld * 2 + 16 * c);
       } else {
-        const int i = u * 8 + (lane >> 3);
-        int c = (lane & 7) ^ ((i >> 1) & 7);
+        constexpr int per = BK / 8;
+        const int i = u * (64 / per) + lane / per;
+        int c = (lane % per) ^ kswz<BK>(i);
         if (8 * c >= klim) c = 0;
         off[j] = (uint32_t)(min(i, ilim - 1) * (int)o.ld * 2 + 16 * c);
       }
     }
   }
-  __device__ __forceinline__ void issue(const char* base, uint32_t lds, int wave) const {
-#pragma unroll
-    for (int j = 0; j < COUNT; ++j) copy16_to_lds_off(base, off[j], lds + (wave * COUNT + j) * 1024);
+  // instruction J of a stage: base its first element, lds the wavefront's part of the tile
+  template <int J>
+  __device__ __forceinline__ void issue(const char* base, uint32_t lds) const {
+    copy16_to_lds_off(base, off[J], lds + J * 1024);
   }
 };
 
-// A wavefront's reads of an operand's tile: FRAGS tiles of 32 rows from row i on.
-template <int I, int FRAGS, bool KOUTER>
+// A wavefront's reads of an operand's tile: FRAGS tiles of 32 rows from row i on, elements 16 KK .. 16 KK + 15 of the stage.
+template <int I, int BK, int FRAGS, bool KOUTER>
 struct Reader {
-  uint32_t at[KOUTER ? FRAGS : 4];
+  uint32_t at[KOUTER ? FRAGS : BK / 16];
   __device__ __forceinline__ Reader(int i, int lane) {
     if (KOUTER) {
       const int l = lane & 15, k = 8 * (lane >> 5) + (l >> 2);
@@ -89,7 +100,7 @@ struct Reader {
     } else {
       const int r = i + (lane & 31);
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) at[kk] = r * BK * 2 + (((2 * kk + (lane >> 5)) ^ ((r >> 1) & 7)) << 4);
+      for (int kk = 0; kk < BK / 16; ++kk) at[kk] = r * BK * 2 + (((2 * kk + (lane >> 5)) ^ kswz<BK>(r)) << 4);
     }
   }
   template <int KK>
@@ -107,12 +118,13 @@ struct Reader {
 };
 
 // acc = A rows i0 .. i0 + M - 1 (down the tiles) x B rows j0 .. j0 + N - 1 (across) over ks elements (all there are, padded to
-// a multiple of 64).  Two stages in LDS: while one is multiplied, the next is copied.  The barrier between two stages
-// stands before the last quarter of a stage's products, whose operands are in registers by then, so that they cover
-// the first reads of the next stage.
-template <class S, bool KA, bool KB>
-__device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Operand& A, const Operand& B, int planes, int64_t i0, int64_t j0,
-                                        int ks, uint8_t* lds) {
+// a multiple of 64).  RING stages in LDS: while one is multiplied, the next RING - 1 are on their way.  The barrier
+// between two stages stands before the last of a stage's products, whose operands are in registers by then, so
+// that they cover the first reads of the next stage.
+template <class S, int PLANES, bool KA, bool KB>
+__device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Operand& A, const Operand& B, int64_t i0, int64_t j0, int ks,
+                                        uint8_t* lds) {
+  constexpr int BK = S::BK, QS = BK / 16;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
   for (int f = 0; f < S::FM; ++f)
@@ -120,60 +132,109 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
     for (int g = 0; g < S::FN; ++g)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[f][g][e] = 0.f;
-  const int nk = (ks + BK - 1) / BK, steps = planes == 3 ? 6 * nk : nk;
+  const int nk = (ks + 63) / 64 * (64 / BK), steps = PLANES == 3 ? 6 * nk : nk;
   if (steps == 0) return;
-  Loader<S::M, S::WAVES, KA> la(A, i0);
-  Loader<S::N, S::WAVES, KB> lb(B, j0);
-  const Reader<S::M, S::FM, KA> ra(wave / S::WN * S::FM * 32, lane);
-  const Reader<S::N, S::FN, KB> rb(wave % S::WN * S::FN * 32, lane);
+  using LA = Loader<S::M, BK, S::WAVES, KA>;
+  using LB = Loader<S::N, BK, S::WAVES, KB>;
+  LA la(A, i0);
+  LB lb(B, j0);
+  const Reader<S::M, BK, S::FM, KA> ra(wave / S::WN * S::FM * 32, lane);
+  const Reader<S::N, BK, S::FN, KB> rb(wave % S::WN * S::FN * 32, lane);
   const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(lds));
-  const bool ragged = min(A.ks, B.ks) < nk * BK;
-  int pair = planes == 3 ? 0 : 5, kt = 0;
+  const int inside = min(A.ks, B.ks), whole = inside / BK;   // stages that lie wholly inside both operands
   la.aim(A, i0, BK, wave, lane);
   lb.aim(B, j0, BK, wave, lane);
-  auto issue = [&](int stage) {
-    if (ragged && (kt == nk - 1 || kt == 0)) {   // (the last stage of a plane, and the first behind it)
-      la.aim(A, i0, min(BK, A.ks - kt * BK), wave, lane);
-      lb.aim(B, j0, min(BK, B.ks - kt * BK), wave, lane);
+  int pair = 0, kt = 0, fill = 0;
+  const char* pa = (const char*)(la.p + (PLANES == 3 ? 2 * A.plane : 0));
+  const char* pb = (const char*)lb.p;
+  const char *qa, *qb;       // the stage that is being copied, and where to
+  uint32_t da, db;
+  auto point = [&] {
+    qa = pa, qb = pb;
+    if (whole < nk && (kt >= whole || kt == 0)) {   // (the last stages of a plane, and the first behind them)
+      int ka = A.ks - kt * BK, kb = B.ks - kt * BK;
+      if (ka <= 0) qa = pa - kt * la.step, ka = A.ks;   // wholly behind the operand's end: its first stage again
+      if (kb <= 0) qb = pb - kt * lb.step, kb = B.ks;
+      la.aim(A, i0, min(BK, ka), wave, lane);
+      lb.aim(B, j0, min(BK, kb), wave, lane);
     }
-    // the planes of A and B by pair: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
-    const int pa = pair == 0 ? 2 : pair == 1 || pair == 3 ? 1 : 0, pb = pair == 2 ? 2 : pair == 1 || pair == 4 ? 1 : 0;
-    la.issue((const char*)(la.p + pa * A.plane) + kt * la.step, at + stage * S::STAGE, wave);
-    lb.issue((const char*)(lb.p + pb * B.plane) + kt * lb.step, at + stage * S::STAGE + S::M * BK * 2, wave);
-    if (++kt == nk) {
+    qa = uniform(qa);
+    qb = uniform(qb);
+    da = at + fill * S::STAGE + wave * LA::COUNT * 1024;
+    db = at + fill * S::STAGE + S::M * BK * 2 + wave * LB::COUNT * 1024;
+    if (++fill == S::RING) fill = 0;
+    ++kt;
+    pa += la.step;
+    pb += lb.step;
+    if (PLANES == 3 && kt == nk) {
       kt = 0;
-      ++pair;
+      ++pair;   // the planes of A and B: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
+      const int ia = pair == 1 || pair == 3 ? 1 : 0, ib = pair == 2 ? 2 : pair == 1 || pair == 4 ? 1 : 0;
+      pa = (const char*)(la.p + ia * A.plane);
+      pb = (const char*)(lb.p + ib * B.plane);
     }
   };
+  constexpr int COPIES = LA::COUNT + LB::COUNT;
+  auto copy = [&](auto j) {
+    constexpr int J = decltype(j)::value;
+    if constexpr (J < LA::COUNT) la.template issue<J>(qa, da);
+    else lb.template issue<J - LA::COUNT>(qb, db);
+  };
+  auto issue = [&] {
+    point();
+    static_for<COPIES>(copy);
+  };
+  // waits until the next stage is in LDS (ahead: RING - 2 later ones have been issued)
+  auto landed = [&](bool ahead) {
+    if (ahead) wait_vmem<(S::RING - 2) * COPIES>();
+    else wait_vmem<0>();
+    barrier_only();
+  };
   bf16x8 fa[2][S::FM], fb[2][S::FN];
-  issue(0);
-  wait_vmem<0>();
-  barrier_only();
-  if (steps > 1) issue(1);
+  for (int s = 0; s < S::RING - 1 && s < steps; ++s) issue();
+  landed(S::RING - 1 <= steps);
+  if (S::RING - 1 < steps) issue();
   ra.template read<0>(fa[0], lds);
   rb.template read<0>(fb[0], lds + S::M * BK * 2);
-  for (int s = 0; s < steps; ++s) {
-    const uint8_t* tile = lds + (s & 1) * S::STAGE;
-    const uint8_t* next = lds + (~s & 1) * S::STAGE;
-    static_for<4>([&](auto q) {
+  int use = 0;
+  // One stage: COPY: a later stage is copied meanwhile, into this one's place; NEXT: a stage follows.
+  auto stage = [&](auto copy_flag, auto next_flag) {
+    constexpr bool COPY = decltype(copy_flag)::value, NEXT = decltype(next_flag)::value;
+    const uint8_t* tile = lds + use * S::STAGE;
+    if (++use == S::RING) use = 0;
+    const uint8_t* next = lds + use * S::STAGE;
+    static_for<QS>([&](auto q) {
       constexpr int KK = decltype(q)::value;
-      if constexpr (KK < 3) {
-        ra.template read<(KK + 1) & 3>(fa[(KK + 1) & 1], tile);
-        rb.template read<(KK + 1) & 3>(fb[(KK + 1) & 1], tile + S::M * BK * 2);
-      } else if (s + 1 < steps) {
+      if constexpr (KK < QS - 1) {
+        ra.template read<(KK + 1) % QS>(fa[(KK + 1) & 1], tile);
+        rb.template read<(KK + 1) % QS>(fb[(KK + 1) & 1], tile + S::M * BK * 2);
+      } else if constexpr (NEXT) {
         wait_lds<0>();
-        wait_vmem<0>();
-        barrier_only();
-        if (s + 2 < steps) issue(s & 1);
+        landed(COPY);
         ra.template read<0>(fa[0], next);
         rb.template read<0>(fb[0], next + S::M * BK * 2);
+        if constexpr (COPY) point();
       }
-#pragma unroll
-      for (int f = 0; f < S::FM; ++f)
-#pragma unroll
-        for (int g = 0; g < S::FN; ++g) acc[f][g] = mfma(fa[KK & 1][f], fb[KK & 1][g], acc[f][g]);
+      sched_fence();   // (the reads stay ahead of the products of what was read before, and the copies among these)
+      static_for<S::FM * S::FN>([&](auto m) {
+        constexpr int I = decltype(m)::value, F = I / S::FN, G = I % S::FN, PER = (COPIES + S::FM * S::FN - 1) / (S::FM * S::FN);
+        acc[F][G] = mfma(fa[KK & 1][F], fb[KK & 1][G], acc[F][G]);
+        if constexpr (COPY && KK == QS - 1) {
+          sched_fence();
+          static_for<PER>([&](auto j) {
+            if constexpr (I * PER + decltype(j)::value < COPIES) copy(IntC<I * PER + decltype(j)::value>{});
+          });
+          sched_fence();
+        }
+      });
+      sched_fence();
     });
-  }
+  };
+  int s = 0;
+  for (; s < steps - S::RING; ++s) stage(Flag<true>{}, Flag<true>{});
+  // (the last RING stages: every one of them has been issued)
+  for (; s < steps - 1; ++s) stage(Flag<false>{}, Flag<true>{});
+  stage(Flag<false>{}, Flag<false>{});
   wait_lds<0>();
   barrier_only();   // (the LDS is the caller's again)
 }
@@ -274,7 +335,7 @@ __global__ __launch_bounds__(256) void wplanes_kernel(LogprobArgs a, int piece) 
 }
 
 // ---- a tile of logits: M entries of the piece down, N rows across
-template <class S, bool BACKWARD>
+template <class S, int PLANES, bool BACKWARD>
 __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -283,7 +344,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;   // the wavefront's first entry and row of the tile
   f32x16 acc[S::FM][S::FN];
   const Operand W = w_operand(a, piece);
-  product<S, false, false>(acc, W, x_operand(a), a.planes, i0, j0, a.hp, lds);
+  product<S, PLANES, false, false>(acc, W, x_operand(a), i0, j0, a.hp, lds);
   const float c = a.scale * kLog2e;
   if constexpr (!BACKWARD) {
     LogprobStat* part = (LogprobStat*)lds;                 // [WM][N]
@@ -354,7 +415,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = iw + 32 * f + down(8 * h + e, lane) < W.rows ? acc[f][g][8 * h + e] * a.scale : 0.f;
           const int i = iw + 32 * f + 16 * h + 8 * (lane >> 5);
-          if (a.planes == 1) {
+          if constexpr (PLANES == 1) {
             const u32x4 y = rows8(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
             if (i < a.piece_v) *(u32x4*)(a.dl + r * a.piece_v + i) = y;
           } else {
@@ -448,7 +509,7 @@ __device__ __forceinline__ void put_rows(void* p, int64_t row, int i, int limit,
 }
 
 // dX: M of the hidden dimension down, N rows across
-template <class S>
+template <class S, int PLANES>
 __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -458,7 +519,7 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
   f32x16 acc[S::FM][S::FN];
   const Operand W = swapped(w_operand(a, piece));
   const Operand D = {a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.np, a.piece_v};
-  product<S, true, false>(acc, W, D, a.planes, i0, j0, W.ks, lds);
+  product<S, PLANES, true, false>(acc, W, D, i0, j0, W.ks, lds);
 #pragma unroll
   for (int g = 0; g < S::FN; ++g) {
     const int64_t r = j0 + jw + 32 * g + (lane & 31);
@@ -480,14 +541,14 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
         }
       }
       const bool last = piece == a.pieces - 1;
-      put_rows(last ? a.dX : (void*)a.dx_acc, row, i, limit, acc[f][g], 0, !last || a.planes == 3, lane);
-      put_rows(last ? a.dX : (void*)a.dx_acc, row, i, limit, acc[f][g], 1, !last || a.planes == 3, lane);
+      put_rows(last ? a.dX : (void*)a.dx_acc, row, i, limit, acc[f][g], 0, !last || PLANES == 3, lane);
+      put_rows(last ? a.dX : (void*)a.dx_acc, row, i, limit, acc[f][g], 1, !last || PLANES == 3, lane);
     }
   }
 }
 
 // dW: M of the hidden dimension down, N entries across
-template <class S>
+template <class S, int PLANES>
 __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -497,15 +558,15 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
   f32x16 acc[S::FM][S::FN];
   const Operand X = {a.xc, a.hp, (int64_t)a.np * a.hp, a.hp, a.np};
   const Operand D = {a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, a.np};
-  product<S, true, true>(acc, X, D, a.planes, i0, j0, a.np, lds);
+  product<S, PLANES, true, true>(acc, X, D, i0, j0, a.np, lds);
 #pragma unroll
   for (int g = 0; g < S::FN; ++g) {
     const int64_t v = j0 + jw + 32 * g + (lane & 31), at = (int64_t)piece * a.piece_v + v;
     const int limit = v < a.piece_v && at < a.v ? a.h : 0;
 #pragma unroll
     for (int f = 0; f < S::FM; ++f) {
-      put_rows(a.dW, at * a.h, iw + 32 * f, limit, acc[f][g], 0, a.planes == 3, lane);
-      put_rows(a.dW, at * a.h, iw + 32 * f, limit, acc[f][g], 1, a.planes == 3, lane);
+      put_rows(a.dW, at * a.h, iw + 32 * f, limit, acc[f][g], 0, PLANES == 3, lane);
+      put_rows(a.dW, at * a.h, iw + 32 * f, limit, acc[f][g], 1, PLANES == 3, lane);
     }
   }
 }
@@ -524,24 +585,43 @@ hipError_t launch_logprob_wplanes(const LogprobArgs& a, int piece, hipStream_t s
   hipLaunchKernelGGL(wplanes_kernel, dim3((unsigned)a.piece_v), dim3(256), 0, st, a, piece);
   return hipGetLastError();
 }
-#define PSATTN_LP_LAUNCH(KERNEL, S, DOWN, ACROSS)                                                                          \
-  do {                                                                                                                   \
-    const int d = tiles(DOWN, S::M), c = tiles(ACROSS, S::N);                                                              \
-    hipLaunchKernelGGL(KERNEL, dim3((unsigned)((int64_t)d * c)), dim3(S::THREADS), 0, st, a, piece, d, c);                  \
-  } while (0)
-
-hipError_t launch_logprob_logits(const LogprobArgs& a, int piece, bool backward, hipStream_t st) {
+namespace {
+// One workgroup per tile of down x across.
+template <class S, class K>
+void launch_tiles(K kernel, int64_t down, int64_t across, const LogprobArgs& a, int piece, hipStream_t st) {
+  const int d = tiles(down, S::M), c = tiles(across, S::N);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)d * c)), dim3(S::THREADS), 0, st, a, piece, d, c);
+}
+template <int PLANES>
+void logits(const LogprobArgs& a, int piece, bool backward, hipStream_t st) {
   const int rows = piece_rows(a, piece);
   if (backward) {
-    if (a.shape == LP_LARGE) PSATTN_LP_LAUNCH((logits_kernel<Large, true>), Large, rows, a.np);
-    else PSATTN_LP_LAUNCH((logits_kernel<Small, true>), Small, rows, a.np);
+    if (a.shape == LP_LARGE) launch_tiles<Large>(logits_kernel<Large, PLANES, true>, rows, a.np, a, piece, st);
+    else launch_tiles<Small>(logits_kernel<Small, PLANES, true>, rows, a.np, a, piece, st);
   } else if (a.shape == LP_LARGE) {
-    PSATTN_LP_LAUNCH((logits_kernel<Large, false>), Large, rows, a.n);
+    launch_tiles<Large>(logits_kernel<Large, PLANES, false>, rows, a.n, a, piece, st);
   } else if (a.shape == LP_SMALL) {
-    PSATTN_LP_LAUNCH((logits_kernel<Small, false>), Small, rows, a.n);
+    launch_tiles<Small>(logits_kernel<Small, PLANES, false>, rows, a.n, a, piece, st);
   } else {
-    PSATTN_LP_LAUNCH((logits_kernel<Thin, false>), Thin, rows, a.n);
+    launch_tiles<Thin>(logits_kernel<Thin, PLANES, false>, rows, a.n, a, piece, st);
   }
+}
+template <int PLANES>
+void dx(const LogprobArgs& a, int piece, hipStream_t st) {
+  if (a.shape == LP_LARGE) launch_tiles<Large>(dx_kernel<Large, PLANES>, a.h, a.n, a, piece, st);
+  else launch_tiles<Small>(dx_kernel<Small, PLANES>, a.h, a.n, a, piece, st);
+}
+template <int PLANES>
+void dw(const LogprobArgs& a, int piece, hipStream_t st) {
+  const int rows = piece_rows(a, piece);
+  if (a.shape == LP_LARGE) launch_tiles<Large>(dw_kernel<Large, PLANES>, a.h, rows, a, piece, st);
+  else launch_tiles<Small>(dw_kernel<Small, PLANES>, a.h, rows, a, piece, st);
+}
+}  // namespace
+
+hipError_t launch_logprob_logits(const LogprobArgs& a, int piece, bool backward, hipStream_t st) {
+  if (a.planes == 3) logits<3>(a, piece, backward, st);
+  else logits<1>(a, piece, backward, st);
   return hipGetLastError();
 }
 hipError_t launch_logprob_finish(const LogprobArgs& a, hipStream_t st) {
@@ -551,15 +631,14 @@ hipError_t launch_logprob_finish(const LogprobArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 hipError_t launch_logprob_dx(const LogprobArgs& a, int piece, hipStream_t st) {
-  if (a.shape == LP_LARGE) PSATTN_LP_LAUNCH(dx_kernel<Large>, Large, a.h, a.n);
-  else PSATTN_LP_LAUNCH(dx_kernel<Small>, Small, a.h, a.n);
+  if (a.planes == 3) dx<3>(a, piece, st);
+  else dx<1>(a, piece, st);
   return hipGetLastError();
 }
 hipError_t launch_logprob_dx_sum(const LogprobArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_logprob_dw(const LogprobArgs& a, int piece, hipStream_t st) {
-  const int rows = piece_rows(a, piece);
-  if (a.shape == LP_LARGE) PSATTN_LP_LAUNCH(dw_kernel<Large>, Large, a.h, rows);
-  else PSATTN_LP_LAUNCH(dw_kernel<Small>, Small, a.h, rows);
+  if (a.planes == 3) dw<3>(a, piece, st);
+  else dw<1>(a, piece, st);
   return hipGetLastError();
 }
 

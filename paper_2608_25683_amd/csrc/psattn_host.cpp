@@ -1078,9 +1078,9 @@ Profiler g_prof;
 const char* kKernelNames[] = {"fwd_main", "fwd_merge",     "bwd_pre", "bwd_kv",   "bwd_dq", "bwd_reduce_kv",
                               "bwd_reduce_dq", "rope",       "kv_scatter", "kv_gather", "split_planes", "silu_bwd",
                               "logprob_prep", "logprob_wplanes", "logprob_logits", "logprob_finish", "logprob_dz", "logprob_dx",
-                              "logprob_dx_sum", "logprob_dw", "adamw_norm", "adamw_scalars", "adamw_step"};
-constexpr int kNumKernels = 23;
-enum { K_LP_PREP = 12, K_LP_WPLANES, K_LP_LOGITS, K_LP_FINISH, K_LP_DZ, K_LP_DX, K_LP_DX_SUM, K_LP_DW, K_ADAMW_NORM, K_ADAMW_SCALARS, K_ADAMW_STEP };
+                              "logprob_dx_sum", "logprob_dw", "logprob_dw_sum", "adamw_norm", "adamw_scalars", "adamw_step"};
+constexpr int kNumKernels = 24;
+enum { K_LP_PREP = 12, K_LP_WPLANES, K_LP_LOGITS, K_LP_FINISH, K_LP_DZ, K_LP_DX, K_LP_DX_SUM, K_LP_DW, K_LP_DW_SUM, K_ADAMW_NORM, K_ADAMW_SCALARS, K_ADAMW_STEP };
 
 hipEvent_t get_event() {
   if (!g_prof.spare.empty()) {
@@ -1340,8 +1340,35 @@ int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 // Everything of the arguments that follows from the sizes, and the workspace: buffers as offsets.
 struct LogprobPlan {
   LogprobArgs a{};
-  size_t part = 0, total = 0, xc = 0, wc = 0, dl = 0, dx_acc = 0, bytes = 0;
+  size_t part = 0, total = 0, xc = 0, wc = 0, dl = 0, dx_acc = 0, dw_acc = 0, bytes = 0;
 };
+
+// The tiles' shape of a product of down x across x k elements, and into how many parts its sum is split.  Estimated time in
+// microseconds: rounds of the workgroups that run at a time, each a start and an end and its stages of 64
+// elements.  Measured: 1.5 a stage for 256 x 256 tiles, 0.83 for two workgroups of 128 x 128 per CU, 0.5 for
+// one with its copies further ahead; parts are written and read as fp32 at 4.5 TB/s behind another launch.  (1280 rows x 1024 x 32000:
+// dX as 80 tiles of 500 stages 315, as seven parts 60; 512 rows x 4096 x 16000: logits 95 large, 67 small, as estimated.)
+struct LogprobTiling { int32_t shape, splits, stages; double us; };
+LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes, int max_splits) {
+  struct Kind { int32_t shape, m, n, slots; double stage, ends; };
+  static const Kind kinds[] = {{LP_LARGE, 256, 256, 256, 1.5, 10}, {LP_SMALL, 128, 128, 512, 0.83, 8}, {LP_DEEP, 128, 128, 256, 0.5, 8}};
+  LogprobTiling best{LP_LARGE, 1, 1, 1e30};
+  const int64_t nk = std::max<int64_t>(1, (k + 63) / 64);
+  for (const Kind& c : kinds) {
+    const int64_t tiles = ((down + c.m - 1) / c.m) * ((across + c.n - 1) / c.n);
+    for (int64_t s = 1; s <= max_splits && s <= nk; ++s) {
+      const int64_t each = (nk + s - 1) / s, parts = (nk + each - 1) / each;
+      if (parts != s) continue;
+      const double r = (double)(tiles * s) / c.slots, rounds = std::ceil(r);
+      const double slabs = (double)s * (double)down * (double)across * 4;
+      if (s > 1 && slabs > (double)((int64_t)512 << 20)) break;
+      const double us = (rounds + std::max(r, 1.0)) / 2 * ((double)each * (planes == 3 ? 6 : 1) * c.stage + c.ends) +
+                        (s > 1 ? 6 + slabs * 2 / 4.5e6 : 0);
+      if (us < best.us) best = {c.shape, (int32_t)s, (int32_t)each, us};
+    }
+  }
+  return best;
+}
 
 psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& p) {
   if (!d) return fail(PSATTN_E_INVALID_ARG, "desc is NULL");
@@ -1374,12 +1401,14 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   const int64_t each = (vr + a.pieces - 1) / a.pieces;
   a.pieces = (int32_t)((vr + each - 1) / each);
   a.piece_v = (int32_t)(256 * each);
-  a.splits = 1;
-  if ((int64_t)(a.n / 32 + 1) * (std::max(a.v, a.h) / 128 + 1) > INT32_MAX)
+  if ((int64_t)(a.n / 32 + 1) * (std::max(a.v, a.h) / 128 + 1) > INT32_MAX / 32)
     return fail(PSATTN_E_UNSUPPORTED, "rows %d x vocab %d: more tiles than a launch holds", a.n, a.v);
-  const int64_t large = (int64_t)((a.n + 255) / 256) * ((a.v + 255) / 256);
-  a.shape = !bwd && a.n <= 32 ? LP_THIN : large >= 256 ? LP_LARGE : LP_SMALL;
+  a.shape = !bwd && a.n <= 32 ? LP_THIN : logprob_tiling(std::min(a.v, a.piece_v), a.n, a.hp, a.planes, 1).shape;
   a.part_v = a.shape == LP_LARGE ? 256 : 128;
+  const LogprobTiling dx = logprob_tiling(a.h, a.n, std::min(a.v, a.piece_v), a.planes, 32);
+  const LogprobTiling dw = logprob_tiling(a.h, std::min(a.v, a.piece_v), a.n, a.planes, 32);
+  a.shape_dx = dx.shape, a.splits_dx = dx.splits, a.stages_dx = dx.stages;
+  a.shape_dw = dw.shape, a.splits_dw = dw.splits, a.stages_dw = dw.stages;
   size_t cur = 0;
   auto take = [&](size_t bytes) {
     const size_t at = cur;
@@ -1394,7 +1423,8 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   } else {
     p.total = take((size_t)a.n * 4);
     p.dl = take((size_t)a.planes * a.np * a.piece_v * 2);
-    if (a.pieces > 1 || a.splits > 1) p.dx_acc = take((size_t)a.splits * a.n * a.h * 4);
+    if (a.pieces > 1 || a.splits_dx > 1) p.dx_acc = take((size_t)a.splits_dx * a.n * a.h * 4);
+    if (a.splits_dw > 1) p.dw_acc = take((size_t)a.splits_dw * a.piece_v * a.h * 4);
   }
   p.bytes = cur;
   return PSATTN_OK;
@@ -1424,7 +1454,8 @@ psattn_status logprob_begin(const psattn_logprob_desc* d, int pass, const void* 
   a.xc = copy ? (uint16_t*)(b + p.xc) : nullptr;
   a.wc = a.planes == 3 ? (uint16_t*)(b + p.wc) : nullptr;
   a.dl = (uint16_t*)(b + p.dl);
-  a.dx_acc = a.pieces > 1 || a.splits > 1 ? (float*)(b + p.dx_acc) : nullptr;
+  a.dx_acc = (float*)(b + p.dx_acc);
+  a.dw_acc = (float*)(b + p.dw_acc);
   return PSATTN_OK;
 }
 
@@ -1483,8 +1514,9 @@ psattn_status psattn_logprob_bwd(const psattn_logprob_desc* desc, const void* X,
     if (s == PSATTN_OK && a.n) s = timed(K_LP_DZ, st, [&] { return launch_logprob_logits(a, i, true, st); });
     if (s == PSATTN_OK && a.dX) s = timed(K_LP_DX, st, [&] { return launch_logprob_dx(a, i, st); });
     if (s == PSATTN_OK && a.dW) s = timed(K_LP_DW, st, [&] { return launch_logprob_dw(a, i, st); });
+    if (s == PSATTN_OK && a.dW && a.splits_dw > 1) s = timed(K_LP_DW_SUM, st, [&] { return launch_logprob_dw_sum(a, i, st); });
   }
-  if (s == PSATTN_OK && a.dX && a.splits > 1) s = timed(K_LP_DX_SUM, st, [&] { return launch_logprob_dx_sum(a, st); });
+  if (s == PSATTN_OK && a.dX && a.splits_dx > 1) s = timed(K_LP_DX_SUM, st, [&] { return launch_logprob_dx_sum(a, st); });
   return s;
 }
 

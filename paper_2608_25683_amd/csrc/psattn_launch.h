@@ -57,13 +57,14 @@ struct BwdArgs {
 struct LogprobStat { float top, sum; };   // max of z log2(e) and the sum of exp2(z log2(e) - max)
 struct LogprobArgs {
   int32_t n, h, v, e;        // rows, hidden, vocabulary, targets
-  int32_t shape;             // LP_THIN .. LP_LARGE
+  int32_t shape, shape_dx, shape_dw;   // LP_THIN .. LP_LARGE: of the logits' tiles, of the gradients'
   int32_t part_v;            // forward: entries per part, those of a tile
   int32_t planes;            // 1: bf16.  3: fp32 as three bf16 planes
   int32_t hp, np;            // h and n rounded up to 64: the padding of xc and dl holds zeros
   int32_t piece_v;           // entries per piece, a multiple of 256
   int32_t pieces;
-  int32_t splits;            // of a piece's entries in the dX product, each with its own fp32 sums
+  int32_t splits_dx, stages_dx;   // parts of a piece's entries in the dX product, each with its own fp32 sums, of so many
+  int32_t splits_dw, stages_dw;   //   stages of 64; parts of the rows in the dW product likewise
   float scale;
   const void* X;
   const void* W;
@@ -80,9 +81,11 @@ struct LogprobArgs {
   uint16_t* xc;              // [planes][np][hp]: X as the products take it; backward: zero in rows that have no gradient
   uint16_t* wc;              // fp32: [planes][piece_v][hp] planes of the piece
   uint16_t* dl;              // backward: [planes][np][piece_v] dz of the piece
-  float* dx_acc;             // backward: [splits][n][h] sums over the pieces, where there is more than one piece or split
+  float* dx_acc;             // backward: [splits_dx][n][h] sums over the pieces, where there is more than one piece or part
+  float* dw_acc;             // backward: [splits_dw][piece_v][h] of a piece, where there is more than one part
 };
-enum { LP_THIN, LP_SMALL, LP_LARGE };   // tiles of 128 x 32, 128 x 128, 256 x 256 (entries or hidden x rows or entries)
+// tiles of 128 x 32, 128 x 128 (one workgroup per CU with more stages in flight, or two), 256 x 256
+enum { LP_THIN, LP_DEEP, LP_SMALL, LP_LARGE };
 
 // AdamW (psattn_adamw.hip)
 struct AdamwTensor {
@@ -190,6 +193,7 @@ PSATTN_WEAK hipError_t launch_logprob_logits(const LogprobArgs& a, int piece, bo
 PSATTN_WEAK hipError_t launch_logprob_finish(const LogprobArgs& a, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_dx(const LogprobArgs& a, int piece, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_dx_sum(const LogprobArgs& a, hipStream_t st);
+PSATTN_WEAK hipError_t launch_logprob_dw_sum(const LogprobArgs& a, int piece, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_dw(const LogprobArgs& a, int piece, hipStream_t st);
 PSATTN_WEAK hipError_t launch_adamw_norm(const AdamwArgs& a, const AdamwGrads& g, hipStream_t st);
 PSATTN_WEAK hipError_t launch_adamw_scalars(const AdamwArgs& a, bool with_norm, hipStream_t st);

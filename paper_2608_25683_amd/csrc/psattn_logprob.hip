@@ -25,6 +25,7 @@ struct Shape2 {
 };
 using Large = Shape2<2, 4, 4, 2, 64, 2>;    // 256 x 256, one workgroup per CU
 using Small = Shape2<2, 2, 2, 2, 64, 2>;    // 128 x 128, two
+using Deep = Shape2<2, 2, 2, 2, 64, 4>;     // 128 x 128, one, three stages ahead
 using Thin = Shape2<4, 1, 1, 1, 64, 2>;     // 128 x 32, four
 
 // An operand of a product: element (i, k) of plane q at p + q plane + i ld + k, or + k ld + i where K is the outer dimension.
@@ -132,7 +133,7 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
     for (int g = 0; g < S::FN; ++g)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[f][g][e] = 0.f;
-  const int nk = (ks + 63) / 64 * (64 / BK), steps = PLANES == 3 ? 6 * nk : nk;
+  const int nk = max(0, ks + 63) / 64 * (64 / BK), steps = PLANES == 3 ? 6 * nk : nk;
   if (steps == 0) return;
   using LA = Loader<S::M, BK, S::WAVES, KA>;
   using LB = Loader<S::N, BK, S::WAVES, KB>;
@@ -268,6 +269,12 @@ __device__ __forceinline__ Operand w_operand(const LogprobArgs& a, int piece) {
   const int v0 = piece * a.piece_v, rows = min(a.piece_v, a.v - v0);
   if (a.wc) return {a.wc, a.hp, (int64_t)a.piece_v * a.hp, rows, a.hp};
   return {(const bf16_t*)a.W + (int64_t)v0 * a.h, a.h, 0, rows, a.h};
+}
+// elements k0 .. k0 + k - 1 of the summed dimension alone
+__device__ __forceinline__ Operand part_of(Operand o, bool kouter, int64_t k0, int k) {
+  o.p += kouter ? k0 * o.ld : k0;
+  o.ks = (int)min((int64_t)k, o.ks - k0);
+  return o;
 }
 __device__ __forceinline__ Operand swapped(const Operand& o) { return {o.p, o.ld, o.plane, o.ks, o.rows}; }
 
@@ -511,15 +518,18 @@ __device__ __forceinline__ void put_rows(void* p, int64_t row, int i, int limit,
 // dX: M of the hidden dimension down, N rows across
 template <class S, int PLANES>
 __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
+  const int split = blockIdx.y, k = a.stages_dx * 64;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Tile tile = tile_of(downs, acrosses, 4);
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
   f32x16 acc[S::FM][S::FN];
-  const Operand W = swapped(w_operand(a, piece));
-  const Operand D = {a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.np, a.piece_v};
+  const Operand W = part_of(swapped(w_operand(a, piece)), true, (int64_t)split * k, k);
+  const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.np, a.piece_v}, false, (int64_t)split * k, k);
   product<S, PLANES, true, false>(acc, W, D, i0, j0, W.ks, lds);
+  const bool last = piece == a.pieces - 1 && a.splits_dx == 1;
+  float* sums = a.dx_acc + (int64_t)split * a.n * a.h;
 #pragma unroll
   for (int g = 0; g < S::FN; ++g) {
     const int64_t r = j0 + jw + 32 * g + (lane & 31);
@@ -534,15 +544,14 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
         for (int q = 0; q < 4; ++q) {
           const int at = i + 8 * q + 4 * (lane >> 5);
           if (at < limit) {
-            const f32x4 y = *(const f32x4*)(a.dx_acc + row + at);
+            const f32x4 y = *(const f32x4*)(sums + row + at);
 #pragma unroll
             for (int k = 0; k < 4; ++k) acc[f][g][4 * q + k] += y[k];
           }
         }
       }
-      const bool last = piece == a.pieces - 1;
-      put_rows(last ? a.dX : (void*)a.dx_acc, row, i, limit, acc[f][g], 0, !last || PLANES == 3, lane);
-      put_rows(last ? a.dX : (void*)a.dx_acc, row, i, limit, acc[f][g], 1, !last || PLANES == 3, lane);
+      put_rows(last ? a.dX : (void*)sums, row, i, limit, acc[f][g], 0, !last || PLANES == 3, lane);
+      put_rows(last ? a.dX : (void*)sums, row, i, limit, acc[f][g], 1, !last || PLANES == 3, lane);
     }
   }
 }
@@ -550,24 +559,39 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
 // dW: M of the hidden dimension down, N entries across
 template <class S, int PLANES>
 __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
+  const int split = blockIdx.y, k = a.stages_dw * 64;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Tile tile = tile_of(downs, acrosses, 4);
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
   f32x16 acc[S::FM][S::FN];
-  const Operand X = {a.xc, a.hp, (int64_t)a.np * a.hp, a.hp, a.np};
-  const Operand D = {a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, a.np};
-  product<S, PLANES, true, true>(acc, X, D, i0, j0, a.np, lds);
+  const Operand X = part_of({a.xc, a.hp, (int64_t)a.np * a.hp, a.hp, a.np}, true, (int64_t)split * k, k);
+  const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, a.np}, true, (int64_t)split * k, k);
+  product<S, PLANES, true, true>(acc, X, D, i0, j0, X.ks, lds);
+  const bool sums = a.splits_dw > 1;
+  void* out = sums ? (void*)(a.dw_acc + (int64_t)split * a.piece_v * a.h) : a.dW;
 #pragma unroll
   for (int g = 0; g < S::FN; ++g) {
     const int64_t v = j0 + jw + 32 * g + (lane & 31), at = (int64_t)piece * a.piece_v + v;
     const int limit = v < a.piece_v && at < a.v ? a.h : 0;
 #pragma unroll
     for (int f = 0; f < S::FM; ++f) {
-      put_rows(a.dW, at * a.h, iw + 32 * f, limit, acc[f][g], 0, PLANES == 3, lane);
-      put_rows(a.dW, at * a.h, iw + 32 * f, limit, acc[f][g], 1, PLANES == 3, lane);
+      put_rows(out, (sums ? v : at) * a.h, iw + 32 * f, limit, acc[f][g], 0, sums || PLANES == 3, lane);
+      put_rows(out, (sums ? v : at) * a.h, iw + 32 * f, limit, acc[f][g], 1, sums || PLANES == 3, lane);
     }
+  }
+}
+
+// out [n] = the sum of the slabs of n fp32 elements, first to last
+template <bool FP32>
+__global__ __launch_bounds__(256) void slabs_kernel(const float* slab, int64_t stride, int count, void* out, int64_t n) {
+  for (int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x); i < n; i += 4 * (int64_t)gridDim.x * 256) {
+    f32x4 x = *(const f32x4*)(slab + i);
+#pragma unroll 4
+    for (int k = 1; k < count; ++k) x += *(const f32x4*)(slab + k * stride + i);
+    if (FP32) *(f32x4*)((float*)out + i) = x;
+    else *(u32x2*)((bf16_t*)out + i) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
   }
 }
 
@@ -586,42 +610,43 @@ hipError_t launch_logprob_wplanes(const LogprobArgs& a, int piece, hipStream_t s
   return hipGetLastError();
 }
 namespace {
-// One workgroup per tile of down x across.
+// One workgroup per tile of down x across and part of the sum.
 template <class S, class K>
-void launch_tiles(K kernel, int64_t down, int64_t across, const LogprobArgs& a, int piece, hipStream_t st) {
+void launch_tiles(K kernel, int64_t down, int64_t across, int parts, const LogprobArgs& a, int piece, hipStream_t st) {
   const int d = tiles(down, S::M), c = tiles(across, S::N);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)d * c)), dim3(S::THREADS), 0, st, a, piece, d, c);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)d * c), (unsigned)parts), dim3(S::THREADS), 0, st, a, piece, d, c);
 }
-template <int PLANES>
-void logits(const LogprobArgs& a, int piece, bool backward, hipStream_t st) {
-  const int rows = piece_rows(a, piece);
-  if (backward) {
-    if (a.shape == LP_LARGE) launch_tiles<Large>(logits_kernel<Large, PLANES, true>, rows, a.np, a, piece, st);
-    else launch_tiles<Small>(logits_kernel<Small, PLANES, true>, rows, a.np, a, piece, st);
-  } else if (a.shape == LP_LARGE) {
-    launch_tiles<Large>(logits_kernel<Large, PLANES, false>, rows, a.n, a, piece, st);
-  } else if (a.shape == LP_SMALL) {
-    launch_tiles<Small>(logits_kernel<Small, PLANES, false>, rows, a.n, a, piece, st);
-  } else {
-    launch_tiles<Thin>(logits_kernel<Thin, PLANES, false>, rows, a.n, a, piece, st);
-  }
+template <int PLANES, bool BACKWARD>
+void logits(const LogprobArgs& a, int piece, hipStream_t st) {
+  const int rows = piece_rows(a, piece), n = BACKWARD ? a.np : a.n;
+  if (a.shape == LP_LARGE) launch_tiles<Large>(logits_kernel<Large, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
+  else if (a.shape == LP_SMALL) launch_tiles<Small>(logits_kernel<Small, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
+  else if (BACKWARD || a.shape == LP_DEEP) launch_tiles<Deep>(logits_kernel<Deep, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
+  else launch_tiles<Thin>(logits_kernel<Thin, PLANES, false>, rows, n, 1, a, piece, st);
 }
 template <int PLANES>
 void dx(const LogprobArgs& a, int piece, hipStream_t st) {
-  if (a.shape == LP_LARGE) launch_tiles<Large>(dx_kernel<Large, PLANES>, a.h, a.n, a, piece, st);
-  else launch_tiles<Small>(dx_kernel<Small, PLANES>, a.h, a.n, a, piece, st);
+  if (a.shape_dx == LP_LARGE) launch_tiles<Large>(dx_kernel<Large, PLANES>, a.h, a.n, a.splits_dx, a, piece, st);
+  else if (a.shape_dx == LP_SMALL) launch_tiles<Small>(dx_kernel<Small, PLANES>, a.h, a.n, a.splits_dx, a, piece, st);
+  else launch_tiles<Deep>(dx_kernel<Deep, PLANES>, a.h, a.n, a.splits_dx, a, piece, st);
 }
 template <int PLANES>
 void dw(const LogprobArgs& a, int piece, hipStream_t st) {
   const int rows = piece_rows(a, piece);
-  if (a.shape == LP_LARGE) launch_tiles<Large>(dw_kernel<Large, PLANES>, a.h, rows, a, piece, st);
-  else launch_tiles<Small>(dw_kernel<Small, PLANES>, a.h, rows, a, piece, st);
+  if (a.shape_dw == LP_LARGE) launch_tiles<Large>(dw_kernel<Large, PLANES>, a.h, rows, a.splits_dw, a, piece, st);
+  else if (a.shape_dw == LP_SMALL) launch_tiles<Small>(dw_kernel<Small, PLANES>, a.h, rows, a.splits_dw, a, piece, st);
+  else launch_tiles<Deep>(dw_kernel<Deep, PLANES>, a.h, rows, a.splits_dw, a, piece, st);
+}
+void sum_slabs(const LogprobArgs& a, const float* slab, int64_t stride, int count, void* out, int64_t n, hipStream_t st) {
+  const dim3 grid((unsigned)std::min<int64_t>((n / 4 + 255) / 256, 8192));
+  if (a.planes == 3) hipLaunchKernelGGL(slabs_kernel<true>, grid, dim3(256), 0, st, slab, stride, count, out, n);
+  else hipLaunchKernelGGL(slabs_kernel<false>, grid, dim3(256), 0, st, slab, stride, count, out, n);
 }
 }  // namespace
 
 hipError_t launch_logprob_logits(const LogprobArgs& a, int piece, bool backward, hipStream_t st) {
-  if (a.planes == 3) logits<3>(a, piece, backward, st);
-  else logits<1>(a, piece, backward, st);
+  if (backward) a.planes == 3 ? logits<3, true>(a, piece, st) : logits<1, true>(a, piece, st);
+  else a.planes == 3 ? logits<3, false>(a, piece, st) : logits<1, false>(a, piece, st);
   return hipGetLastError();
 }
 hipError_t launch_logprob_finish(const LogprobArgs& a, hipStream_t st) {
@@ -635,7 +660,15 @@ hipError_t launch_logprob_dx(const LogprobArgs& a, int piece, hipStream_t st) {
   else dx<1>(a, piece, st);
   return hipGetLastError();
 }
-hipError_t launch_logprob_dx_sum(const LogprobArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_logprob_dx_sum(const LogprobArgs& a, hipStream_t st) {
+  sum_slabs(a, a.dx_acc, (int64_t)a.n * a.h, a.splits_dx, a.dX, (int64_t)a.n * a.h, st);
+  return hipGetLastError();
+}
+hipError_t launch_logprob_dw_sum(const LogprobArgs& a, int piece, hipStream_t st) {
+  const int64_t at = (int64_t)piece * a.piece_v * a.h * (a.planes == 3 ? 4 : 2);
+  sum_slabs(a, a.dw_acc, (int64_t)a.piece_v * a.h, a.splits_dw, (uint8_t*)a.dW + at, (int64_t)piece_rows(a, piece) * a.h, st);
+  return hipGetLastError();
+}
 hipError_t launch_logprob_dw(const LogprobArgs& a, int piece, hipStream_t st) {
   if (a.planes == 3) dw<3>(a, piece, st);
   else dw<1>(a, piece, st);

@@ -1340,7 +1340,7 @@ int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 // Everything of the arguments that follows from the sizes, and the workspace: buffers as offsets.
 struct LogprobPlan {
   LogprobArgs a{};
-  size_t part = 0, total = 0, xc = 0, wc = 0, dl = 0, dx_acc = 0, dw_acc = 0, bytes = 0;
+  size_t part = 0, total = 0, xc = 0, wc = 0, dl = 0, dx_acc = 0, dw_acc = 0, ent_row = 0, ent_rem = 0, bytes = 0;
 };
 
 // The tiles' shape of a product of down x across x k elements, and into how many parts its sum is split.  Estimated time in
@@ -1422,6 +1422,10 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
     p.part = take((size_t)((a.v + a.part_v - 1) / a.part_v) * a.n * sizeof(LogprobStat));
   } else {
     p.total = take((size_t)a.n * 4);
+    if (!fp32) {
+      p.ent_row = take((size_t)a.e * 4);
+      p.ent_rem = take((size_t)a.e * 4);
+    }
     p.dl = take((size_t)a.planes * a.np * a.piece_v * 2);
     if (a.pieces > 1 || a.splits_dx > 1) p.dx_acc = take((size_t)a.splits_dx * a.n * a.h * 4);
     if (a.splits_dw > 1) p.dw_acc = take((size_t)a.splits_dw * a.piece_v * a.h * 4);
@@ -1454,6 +1458,8 @@ psattn_status logprob_begin(const psattn_logprob_desc* d, int pass, const void* 
   a.xc = copy ? (uint16_t*)(b + p.xc) : nullptr;
   a.wc = a.planes == 3 ? (uint16_t*)(b + p.wc) : nullptr;
   a.dl = (uint16_t*)(b + p.dl);
+  a.ent_row = (int32_t*)(b + p.ent_row);
+  a.ent_rem = (float*)(b + p.ent_rem);
   a.dx_acc = (float*)(b + p.dx_acc);
   a.dw_acc = (float*)(b + p.dw_acc);
   return PSATTN_OK;

@@ -78,6 +78,8 @@ struct LogprobArgs {
   void* dW;
   LogprobStat* part;         // forward: [parts of the vocabulary][n]
   float* total;              // backward: [n] sum of a row's live dlogp
+  int32_t* ent_row;          // backward, bf16: [e] the row of each target
+  float* ent_rem;            //   and what the rounding of its dz to bf16 left out (at a row's first target of the token; else 0)
   uint16_t* xc;              // [planes][np][hp]: X as the products take it; backward: zero in rows that have no gradient
   uint16_t* wc;              // fp32: [planes][piece_v][hp] planes of the piece
   uint16_t* dl;              // backward: [planes][np][piece_v] dz of the piece

@@ -249,6 +249,31 @@ __device__ __forceinline__ u32x4 rows8(uint32_t a0, uint32_t a1, uint32_t b0, ui
   return u32x4{(uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]};
 }
 
+// A workgroup's tile as bf16 to out [rows across][elements down] (ld elements apart), through LDS, so that whole rows of
+// it leave together: eight(f, g, h) are the 8 elements that rows8 gives the lane for rows 16 h of tile (f, g).  lim_across
+// and lim_down (a multiple of 8): what there is of the tile.
+template <class S, class F>
+__device__ __forceinline__ void store_tile(F&& eight, bf16_t* out, int64_t ld, int64_t lim_across, int64_t lim_down, uint8_t* lds) {
+  constexpr int CH = S::M / 8;   // chunks of 16 bytes in a row, at position c ^ (row mod CH): no two lanes of a write in one bank
+  static_assert(S::M * S::N * 2 <= S::LDS, "the tile fits");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int g = 0; g < S::FN; ++g)
+#pragma unroll
+    for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int j = (wave % S::WN * S::FN + g) * 32 + (lane & 31), c = (wave / S::WN * S::FM + f) * 4 + 2 * h + (lane >> 5);
+        *(u32x4*)(lds + j * S::M * 2 + ((c ^ (j % CH)) << 4)) = eight(f, g, h);
+      }
+  __syncthreads();
+#pragma unroll 8
+  for (int k = threadIdx.x; k < S::N * CH; k += S::THREADS) {
+    const int j = k / CH, c = (k % CH) ^ (j % CH);
+    if (j < lim_across && 8 * c < lim_down) *(u32x4*)(out + j * ld + 8 * c) = ld16(lds + k * 16);
+  }
+}
+
 // Which tile a workgroup takes.  Workgroups go to the 8 XCDs in turn; those of one XCD take consecutive tiles, in bands of
 // `band` tiles down by all tiles across, so that the 32 that run on it at a time share rows of both operands in its L2.
 struct Tile { int down, across; };
@@ -308,6 +333,10 @@ __global__ __launch_bounds__(256) void prep_kernel(LogprobArgs a, int backward) 
         if (t >= 0 && t < a.v) {
           total += g;
           live = live || g != 0.f;
+        }
+        if (!FP32) {
+          a.ent_row[e] = r;
+          a.ent_rem[e] = 0.f;
         }
       }
       a.total[r] = total;
@@ -412,30 +441,61 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
           for (int e = 0; e < 16; ++e)
             if (at == 32 * f + down(e, lane)) acc[f][g][e] += d;
       }
-      if (r >= a.np) continue;
-      const int64_t plane = (int64_t)a.np * a.piece_v;
 #pragma unroll
       for (int f = 0; f < S::FM; ++f)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float x[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = iw + 32 * f + down(8 * h + e, lane) < W.rows ? acc[f][g][8 * h + e] * a.scale : 0.f;
-          const int i = iw + 32 * f + 16 * h + 8 * (lane >> 5);
-          if constexpr (PLANES == 1) {
-            const u32x4 y = rows8(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
-            if (i < a.piece_v) *(u32x4*)(a.dl + r * a.piece_v + i) = y;
-          } else {
-            uint32_t p[3][8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) split3(x[e], p[0][e], p[1][e], p[2][e]);
-#pragma unroll
-            for (int q = 0; q < 3; ++q) {
-              const u32x4 y = rows8(p[q][0] | p[q][1] << 16, p[q][2] | p[q][3] << 16, p[q][4] | p[q][5] << 16, p[q][6] | p[q][7] << 16);
-              if (i < a.piece_v) *(u32x4*)(a.dl + q * plane + r * a.piece_v + i) = y;
-            }
+        for (int e = 0; e < 16; ++e) acc[f][g][e] = iw + 32 * f + down(e, lane) < W.rows ? acc[f][g][e] * a.scale : 0.f;
+      if (PLANES == 1) {
+        // A target's dz is most of its row's, so its rounding would be most of the gradients' error: what it leaves out
+        // goes into them by itself.
+        for (int t = e0; __any(t < e1); ++t) {
+          int at = -1;
+          if (t < e1) {
+            const int v = a.tgt[t];
+            at = v < 0 || v >= a.v ? -1 : v - v0 - iw;
+            for (int u = e0; u < t; ++u)
+              if (a.tgt[u] == v) at = -1;
           }
+          if (!__any(at >= 0 && at < 32 * S::FM)) continue;
+          float x = 0.f;
+          bool mine = false;
+#pragma unroll
+          for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (at == 32 * f + down(e, lane)) x = acc[f][g][e], mine = true;
+          if (mine) a.ent_rem[t] = is_finite(x) ? x - bf2f(pack2(x, 0.f) & 0xffffu) : 0.f;
         }
+      }
+    }
+    bf16_t* out = a.dl + j0 * a.piece_v + i0;
+    const int64_t lim_across = a.np - j0, lim_down = a.piece_v - i0;
+    if constexpr (PLANES == 1) {
+      store_tile<S>(
+          [&](int f, int g, int h) {
+            const f32x16& x = acc[f][g];
+            return rows8(pack2(x[8 * h], x[8 * h + 1]), pack2(x[8 * h + 2], x[8 * h + 3]), pack2(x[8 * h + 4], x[8 * h + 5]),
+                         pack2(x[8 * h + 6], x[8 * h + 7]));
+          },
+          out, a.piece_v, lim_across, lim_down, lds);
+    } else {
+      static_for<3>([&](auto q) {
+        constexpr int Q = decltype(q)::value;
+        if (Q) __syncthreads();
+        store_tile<S>(
+            [&](int f, int g, int h) {
+              uint32_t w[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                uint32_t lo[3], hi[3];
+                split3(acc[f][g][8 * h + 2 * k], lo[0], lo[1], lo[2]);
+                split3(acc[f][g][8 * h + 2 * k + 1], hi[0], hi[1], hi[2]);
+                w[k] = lo[Q] | hi[Q] << 16;
+              }
+              return rows8(w[0], w[1], w[2], w[3]);
+            },
+            out + Q * (int64_t)a.np * a.piece_v, a.piece_v, lim_across, lim_down, lds);
+      });
     }
   }
 }
@@ -498,29 +558,57 @@ __global__ __launch_bounds__(256) void finish_kernel(LogprobArgs a) {
   }
 }
 
-// 8 elements x of a row that the lane holds after rows8's exchange (16 rows of the tile, 8 values of this lane) to p + at in
-// the inputs' type
-__device__ __forceinline__ void put_rows(void* p, int64_t row, int i, int limit, const f32x16& x, int h, bool fp32, int lane) {
-  const int b = 8 * h;
-  if (fp32) {
+// 32 rows of the tile, 4 consecutive ones at a time, as fp32 to p + i .. (those below limit)
+__device__ __forceinline__ void put_rows(float* p, int i, int limit, const f32x16& x, int lane) {
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int at = i + 16 * h + 8 * q + 4 * (lane >> 5);
-      if (at < limit) *(f32x4*)((float*)p + row + at) = f32x4{x[b + 4 * q], x[b + 4 * q + 1], x[b + 4 * q + 2], x[b + 4 * q + 3]};
-    }
+  for (int q = 0; q < 4; ++q) {
+    const int at = i + 8 * q + 4 * (lane >> 5);
+    if (at < limit) *(f32x4*)(p + at) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+  }
+}
+// x += w times the same elements of a bf16 row
+__device__ __forceinline__ void add_rows(f32x16& x, float w, const bf16_t* p, int i, int limit, int lane) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int at = i + 8 * q + 4 * (lane >> 5);
+    if (at >= limit) continue;
+    const u32x2 b = ld8(p + at);
+    x[4 * q] = fmaf(w, bf2f(b[0] & 0xffffu), x[4 * q]);
+    x[4 * q + 1] = fmaf(w, __uint_as_float(b[0] & 0xffff0000u), x[4 * q + 1]);
+    x[4 * q + 2] = fmaf(w, bf2f(b[1] & 0xffffu), x[4 * q + 2]);
+    x[4 * q + 3] = fmaf(w, __uint_as_float(b[1] & 0xffff0000u), x[4 * q + 3]);
+  }
+}
+// the workgroup's tile to a result of the inputs' type
+template <class S, int PLANES>
+__device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::FM][S::FN], void* out, int64_t at, int64_t ld, int64_t lim_across, int64_t lim_down,
+                                         uint8_t* lds) {
+  if constexpr (PLANES == 1) {
+    store_tile<S>(
+        [&](int f, int g, int h) {
+          const f32x16& x = acc[f][g];
+          return rows8(pack2(x[8 * h], x[8 * h + 1]), pack2(x[8 * h + 2], x[8 * h + 3]), pack2(x[8 * h + 4], x[8 * h + 5]),
+                       pack2(x[8 * h + 6], x[8 * h + 7]));
+        },
+        (bf16_t*)out + at, ld, lim_across, lim_down, lds);
   } else {
-    const u32x4 y = rows8(pack2(x[b], x[b + 1]), pack2(x[b + 2], x[b + 3]), pack2(x[b + 4], x[b + 5]), pack2(x[b + 6], x[b + 7]));
-    const int at = i + 16 * h + 8 * (lane >> 5);
-    if (at < limit) *(u32x4*)((bf16_t*)p + row + at) = y;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int g = 0; g < S::FN; ++g) {
+      const int j = (wave % S::WN * S::FN + g) * 32 + (lane & 31);
+#pragma unroll
+      for (int f = 0; f < S::FM; ++f)
+        put_rows((float*)out + at + j * ld, (wave / S::WN * S::FM + f) * 32, j < lim_across ? (int)min(lim_down, (int64_t)S::M) : 0, acc[f][g], lane);
+    }
   }
 }
 
 // dX: M of the hidden dimension down, N rows across
 template <class S, int PLANES>
 __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
-  const int split = blockIdx.y, k = a.stages_dx * 64;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.y, k = a.stages_dx * 64;
   const Tile tile = tile_of(downs, acrosses, 4);
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
@@ -528,40 +616,49 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
   const Operand W = part_of(swapped(w_operand(a, piece)), true, (int64_t)split * k, k);
   const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.np, a.piece_v}, false, (int64_t)split * k, k);
   product<S, PLANES, true, false>(acc, W, D, i0, j0, W.ks, lds);
-  const bool last = piece == a.pieces - 1 && a.splits_dx == 1;
+  const bool last = piece == a.pieces - 1;
   float* sums = a.dx_acc + (int64_t)split * a.n * a.h;
 #pragma unroll
   for (int g = 0; g < S::FN; ++g) {
     const int64_t r = j0 + jw + 32 * g + (lane & 31);
-    const bool in = r < a.n;
-    const int limit = in ? a.h : 0;
-    const int64_t row = r * a.h;
+    const int limit = r < a.n ? a.h : 0;
+    if (piece) {
 #pragma unroll
-    for (int f = 0; f < S::FM; ++f) {
-      const int i = iw + 32 * f;
-      if (piece) {
+      for (int f = 0; f < S::FM; ++f)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int at = i + 8 * q + 4 * (lane >> 5);
-          if (at < limit) {
-            const f32x4 y = *(const f32x4*)(sums + row + at);
+          const int at = iw + 32 * f + 8 * q + 4 * (lane >> 5);
+          if (at >= limit) continue;
+          const f32x4 y = *(const f32x4*)(sums + r * a.h + at);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) acc[f][g][4 * q + k] += y[k];
-          }
+          for (int e = 0; e < 4; ++e) acc[f][g][4 * q + e] += y[e];
         }
+    }
+    if (PLANES == 1 && last && split == 0) {   // what the targets' dz left out
+      int e0 = 0, e1 = 0;
+      if (limit) targets_of(a, (int)r, e0, e1);
+      for (int e = e0; e < e1; ++e) {
+        const float rem = a.ent_rem[e];
+        if (rem == 0.f) continue;
+        const bf16_t* w = (const bf16_t*)a.W + (int64_t)a.tgt[e] * a.h;
+#pragma unroll
+        for (int f = 0; f < S::FM; ++f) add_rows(acc[f][g], rem, w, iw + 32 * f, limit, lane);
       }
-      put_rows(last ? a.dX : (void*)sums, row, i, limit, acc[f][g], 0, !last || PLANES == 3, lane);
-      put_rows(last ? a.dX : (void*)sums, row, i, limit, acc[f][g], 1, !last || PLANES == 3, lane);
+    }
+    if (!last || a.splits_dx > 1) {
+#pragma unroll
+      for (int f = 0; f < S::FM; ++f) put_rows(sums + r * a.h, iw + 32 * f, limit, acc[f][g], lane);
     }
   }
+  if (last && a.splits_dx == 1) put_tile<S, PLANES>(acc, a.dX, j0 * a.h + i0, a.h, a.n - j0, a.h - i0, lds);
 }
 
 // dW: M of the hidden dimension down, N entries across
 template <class S, int PLANES>
 __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
-  const int split = blockIdx.y, k = a.stages_dw * 64;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int split = blockIdx.y, k = a.stages_dw * 64;
   const Tile tile = tile_of(downs, acrosses, 4);
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
@@ -569,17 +666,51 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
   const Operand X = part_of({a.xc, a.hp, (int64_t)a.np * a.hp, a.hp, a.np}, true, (int64_t)split * k, k);
   const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, a.np}, true, (int64_t)split * k, k);
   product<S, PLANES, true, true>(acc, X, D, i0, j0, X.ks, lds);
-  const bool sums = a.splits_dw > 1;
-  void* out = sums ? (void*)(a.dw_acc + (int64_t)split * a.piece_v * a.h) : a.dW;
+  const int v0 = piece * a.piece_v + (int)j0, vn = min(S::N, min(a.piece_v - (int)j0, a.v - v0));   // the tile's entries
+  if (PLANES == 1 && split == 0) {
+    // What the targets' dz left out: the targets are looked through for this tile's entries, 64 per wavefront and turn, and
+    // taken in their order.
+    constexpr int TURNS = 8, WORDS = TURNS * S::WAVES;
+    uint64_t* found = (uint64_t*)lds;
+    for (int base = 0; base < a.e; base += 64 * WORDS) {
+      if (base) __syncthreads();
 #pragma unroll
-  for (int g = 0; g < S::FN; ++g) {
-    const int64_t v = j0 + jw + 32 * g + (lane & 31), at = (int64_t)piece * a.piece_v + v;
-    const int limit = v < a.piece_v && at < a.v ? a.h : 0;
+      for (int u = 0; u < TURNS; ++u) {
+        const int e = base + (wave * TURNS + u) * 64 + lane, t = e < a.e ? a.tgt[e] : -1;
+        const uint64_t mask = __ballot(t >= v0 && t < v0 + vn);
+        if (lane == 0) found[wave * TURNS + u] = mask;
+      }
+      __syncthreads();
+      for (int w = 0; w < WORDS && base + 64 * w < a.e; ++w) {
+        for (uint64_t mask = found[w]; mask; mask &= mask - 1) {
+          const int e = base + 64 * w + __builtin_ctzll(mask), j = a.tgt[e] - v0 - jw, r = a.ent_row[e];
+          // (a target that no row lists has no row here)
+          if (j < 0 || j >= 32 * S::FN || r < 0 || r >= a.n) continue;
+          int e0, e1;
+          targets_of(a, r, e0, e1);
+          const float rem = e >= e0 && e < e1 ? a.ent_rem[e] : 0.f;
+          if (rem == 0.f) continue;
 #pragma unroll
-    for (int f = 0; f < S::FM; ++f) {
-      put_rows(out, (sums ? v : at) * a.h, iw + 32 * f, limit, acc[f][g], 0, sums || PLANES == 3, lane);
-      put_rows(out, (sums ? v : at) * a.h, iw + 32 * f, limit, acc[f][g], 1, sums || PLANES == 3, lane);
+          for (int g = 0; g < S::FN; ++g)
+            if (j == 32 * g + (lane & 31)) {
+#pragma unroll
+              for (int f = 0; f < S::FM; ++f) add_rows(acc[f][g], rem, a.xc + (int64_t)r * a.hp, iw + 32 * f, a.h, lane);
+            }
+        }
+      }
     }
+    __syncthreads();
+  }
+  if (a.splits_dw > 1) {
+    float* sums = a.dw_acc + (int64_t)split * a.piece_v * a.h;
+#pragma unroll
+    for (int g = 0; g < S::FN; ++g) {
+      const int j = jw + 32 * g + (lane & 31);
+#pragma unroll
+      for (int f = 0; f < S::FM; ++f) put_rows(sums + (j0 + j) * a.h, iw + 32 * f, j < vn ? a.h : 0, acc[f][g], lane);
+    }
+  } else {
+    put_tile<S, PLANES>(acc, a.dW, (int64_t)v0 * a.h + i0, a.h, vn, a.h - i0, lds);
   }
 }
 

@@ -640,10 +640,10 @@ def _logprob_ws(desc, pass_, ws, X):
     return ws
 
 
-def psattn_logprob_workspace_size(rows: int, hidden: int, vocab: int, dtype: str = "bf16", pass_: int = 0) -> int:
+def psattn_logprob_workspace_size(rows: int, targets: int, hidden: int, vocab: int, dtype: str = "bf16", pass_: int = 0) -> int:
     """Workspace bytes of psattn_logprob_fwd (pass 0) or psattn_logprob_bwd (1)."""
     n = ctypes.c_size_t()
-    desc = LogprobDesc(int(rows), 0, int(hidden), int(vocab), 1.0, PSATTN_BF16 if dtype == "bf16" else PSATTN_FP32)
+    desc = LogprobDesc(int(rows), int(targets), int(hidden), int(vocab), 1.0, PSATTN_BF16 if dtype == "bf16" else PSATTN_FP32)
     _check(lib().psattn_logprob_workspace_size(ctypes.byref(desc), int(pass_), ctypes.byref(n)))
     return n.value
 

@@ -220,7 +220,7 @@ def test_repeats_bitwise_and_leaves_what_is_not_its_own():
     held = []
     for _ in range(3):
         logp, lse, dx, dw = room(tgt.numel()), room(333), room(x.numel(), x.dtype), room(w.numel(), x.dtype)
-        ws = torch.full((P.psattn_logprob_workspace_size(333, 136, 1030, "bf16", 1) + 256,), 0xEE, dtype=torch.uint8, device="cuda")
+        ws = torch.full((P.psattn_logprob_workspace_size(333, tgt.numel(), 136, 1030, "bf16", 1) + 256,), 0xEE, dtype=torch.uint8, device="cuda")
         n = ws.numel() - 256
         P.psattn_logprob_fwd(x, w, ptr, tgt, logp=logp[:-64], LSE=lse[:-64], ws=ws[:n])
         P.psattn_logprob_bwd(x, w, ptr, tgt, lse[:-64], g, dX=dx[:-64].view_as(x), dW=dw[:-64].view_as(w), ws=ws[:n])

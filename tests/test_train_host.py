@@ -60,10 +60,10 @@ def test_logprob_workspace_keeps_no_logits():
     """Under the logits' own bytes wherever these are large, and within what its pieces and sums need."""
     for rows, hidden, vocab in [(20480, 4096, 128256), (8192, 4096, 128256), (100000, 1024, 256000), (1, 4096, 128256), (1, 8, 1)]:
         for dtype, size in (("bf16", 2), ("fp32", 4)):
-            f, b = (P.psattn_logprob_workspace_size(rows, hidden, vocab, dtype, k) for k in (0, 1))
+            f, b = (P.psattn_logprob_workspace_size(rows, rows, hidden, vocab, dtype, k) for k in (0, 1))
             if rows * vocab * 4 > 4 << 30:
                 assert f < rows * vocab * 4 / 4 and b < rows * vocab * 4 / 2, (rows, vocab, dtype, f, b)
-    assert P.psattn_logprob_workspace_size(0, 64, 100, "bf16", 0) >= 0
+    assert P.psattn_logprob_workspace_size(0, 0, 64, 100, "bf16", 0) >= 0
 
 
 def _tensor(**kw):

@@ -1340,7 +1340,7 @@ int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
 // Everything of the arguments that follows from the sizes, and the workspace: buffers as offsets.
 struct LogprobPlan {
   LogprobArgs a{};
-  size_t part = 0, total = 0, xc = 0, wc = 0, dl = 0, dx_acc = 0, dw_acc = 0, ent_row = 0, ent_rem = 0, bytes = 0;
+  size_t part = 0, row = 0, xc = 0, wc = 0, dl = 0, dx_acc = 0, dw_acc = 0, ent_row = 0, ent_rem = 0, bytes = 0;
 };
 
 // The tiles' shape of a product of down x across x k elements, and into how many parts its sum is split.  Estimated time in
@@ -1421,7 +1421,7 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   if (!bwd) {
     p.part = take((size_t)((a.v + a.part_v - 1) / a.part_v) * a.n * sizeof(LogprobStat));
   } else {
-    p.total = take((size_t)a.n * 4);
+    p.row = take((size_t)a.np * sizeof(LogprobRow));
     if (!fp32) {
       p.ent_row = take((size_t)a.e * 4);
       p.ent_rem = take((size_t)a.e * 4);
@@ -1453,7 +1453,7 @@ psattn_status logprob_begin(const psattn_logprob_desc* d, int pass, const void* 
   a.tgt = tgt;
   char* b = (char*)ws;
   a.part = (LogprobStat*)(b + p.part);
-  a.total = (float*)(b + p.total);
+  a.row = (LogprobRow*)(b + p.row);
   const bool copy = pass == 1 || a.planes == 3 || a.h != a.hp;
   a.xc = copy ? (uint16_t*)(b + p.xc) : nullptr;
   a.wc = a.planes == 3 ? (uint16_t*)(b + p.wc) : nullptr;

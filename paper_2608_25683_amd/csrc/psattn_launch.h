@@ -55,6 +55,8 @@ struct BwdArgs {
 // Log-probabilities over a vocabulary (psattn_logprob.hip).  The vocabulary is taken in pieces of piece_v
 // entries (the forward of bf16 in one); buffers in the workspace:
 struct LogprobStat { float top, sum; };   // max of z log2(e) and the sum of exp2(z log2(e) - max)
+// What the backward's tiles take of a row: its G, its LSE log2(e), its targets e0 .. e1 - 1 and, if it is live, the first of them.
+struct LogprobRow { float total, lse2, g0; int32_t t0, e0, e1, pad[2]; };
 struct LogprobArgs {
   int32_t n, h, v, e;        // rows, hidden, vocabulary, targets
   int32_t shape, shape_dx, shape_dw;   // LP_THIN .. LP_LARGE: of the logits' tiles, of the gradients'
@@ -77,7 +79,7 @@ struct LogprobArgs {
   void* dX;
   void* dW;
   LogprobStat* part;         // forward: [parts of the vocabulary][n]
-  float* total;              // backward: [n] sum of a row's live dlogp
+  LogprobRow* row;           // backward: [np]
   int32_t* ent_row;          // backward, bf16: [e] the row of each target
   float* ent_rem;            //   and what the rounding of its dz to bf16 left out (at a row's first target of the token; else 0)
   uint16_t* xc;              // [planes][np][hp]: X as the products take it; backward: zero in rows that have no gradient

@@ -239,8 +239,8 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
   wait_lds<0>();
   barrier_only();   // (the LDS is the caller's again)
 }
-// the row down the 32 x 32 tile of element e of a lane
-__device__ __forceinline__ int down(int e, int lane) { return 8 * (e / 4) + 4 * (lane >> 5) + e % 4; }
+// The row down the 32 x 32 tile of element e of a lane is down(e) + 4 (lane >> 5).
+__device__ __forceinline__ constexpr int down(int e) { return 8 * (e / 4) + e % 4; }
 // The four dwords of bf16 that lanes l and l + 32 hold of tile rows 16 h .. 16 h + 15, as 8 consecutive rows each: lanes below
 // 32 get rows 16 h .., the others 16 h + 8 ..
 __device__ __forceinline__ u32x4 rows8(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1) {
@@ -267,7 +267,7 @@ __device__ __forceinline__ void store_tile(F&& eight, bf16_t* out, int64_t ld, i
         *(u32x4*)(lds + j * S::M * 2 + ((c ^ (j % CH)) << 4)) = eight(f, g, h);
       }
   __syncthreads();
-#pragma unroll 8
+#pragma unroll 4
   for (int k = threadIdx.x; k < S::N * CH; k += S::THREADS) {
     const int j = k / CH, c = (k % CH) ^ (j % CH);
     if (j < lim_across && 8 * c < lim_down) *(u32x4*)(out + j * ld + 8 * c) = ld16(lds + k * 16);
@@ -322,26 +322,29 @@ __global__ __launch_bounds__(256) void prep_kernel(LogprobArgs a, int backward) 
   const int r = blockIdx.x;
   __shared__ int s_live;
   if (threadIdx.x == 0) {
-    bool live = !backward;
-    float total = 0.f;
-    if (backward && r < a.n) {
-      int e0, e1;
-      targets_of(a, r, e0, e1);
-      for (int e = e0; e < e1; ++e) {
-        const int t = a.tgt[e];
-        const float g = a.dlogp[e];
-        if (t >= 0 && t < a.v) {
-          total += g;
-          live = live || g != 0.f;
+    bool live = !backward && r < a.n;
+    if (backward) {
+      LogprobRow row = {0.f, 0.f, 0.f, -1, 0, 0, {0, 0}};
+      if (r < a.n) {
+        targets_of(a, r, row.e0, row.e1);
+        for (int e = row.e0; e < row.e1; ++e) {
+          const int t = a.tgt[e];
+          const float g = a.dlogp[e];
+          if (t >= 0 && t < a.v) {
+            row.total += g;
+            live = live || g != 0.f;
+            if (e == row.e0) row.t0 = t, row.g0 = g;
+          }
+          if (!FP32) {
+            a.ent_row[e] = r;
+            a.ent_rem[e] = 0.f;
+          }
         }
-        if (!FP32) {
-          a.ent_row[e] = r;
-          a.ent_rem[e] = 0.f;
-        }
+        row.lse2 = a.lse[r] * kLog2e;
       }
-      a.total[r] = total;
+      a.row[r] = row;
     }
-    s_live = live && r < a.n;
+    s_live = live;
   }
   __syncthreads();
   const bool live = s_live;
@@ -380,8 +383,13 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;   // the wavefront's first entry and row of the tile
   f32x16 acc[S::FM][S::FN];
   const Operand W = w_operand(a, piece);
+  __shared__ LogprobRow s_row[BACKWARD ? S::N : 1];        // (here so that its reads' time passes under the products)
+  if constexpr (BACKWARD)
+    for (int j = threadIdx.x; j < S::N; j += S::THREADS)
+      if (j0 + j < a.np) s_row[j] = a.row[j0 + j];
   product<S, PLANES, false, false>(acc, W, x_operand(a), i0, j0, a.hp, lds);
   const float c = a.scale * kLog2e;
+  const int left = W.rows - iw - 4 * (lane >> 5);   // element (f, e) is an entry where 32 f + down(e) is below
   if constexpr (!BACKWARD) {
     LogprobStat* part = (LogprobStat*)lds;                 // [WM][N]
 #pragma unroll
@@ -391,7 +399,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
       for (int f = 0; f < S::FM; ++f)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const bool in = iw + 32 * f + down(e, lane) < W.rows;
+          const bool in = 32 * f + down(e) < left;
           acc[f][g][e] = in ? acc[f][g][e] * c : kNegInf;
           top = fmaxf(top, acc[f][g][e]);
         }
@@ -416,54 +424,49 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
     const int v0 = piece * a.piece_v;
 #pragma unroll
     for (int g = 0; g < S::FN; ++g) {
-      const int64_t r = j0 + jw + 32 * g + (lane & 31);
-      const bool in_row = r < a.n;
-      const float total = in_row ? a.total[r] : 0.f, lse2 = in_row ? a.lse[r] * kLog2e : 0.f;
-      int e0 = 0, e1 = 0;
-      if (in_row) targets_of(a, (int)r, e0, e1);
+      sched_fence();
+      LogprobRow row = {0.f, 0.f, 0.f, -1, 0, 0, {0, 0}};
+      if (j0 + jw + 32 * g < a.np) row = s_row[jw + 32 * g + (lane & 31)];
 #pragma unroll
       for (int f = 0; f < S::FM; ++f)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[f][g][e] = total != 0.f ? -total * fast_exp2(acc[f][g][e] * c - lse2) : 0.f;
-      // the targets among the wavefront's entries: few, so each is looked for in the registers
-      for (int t = e0; __any(t < e1); ++t) {
-        int at = -1;
-        float d = 0.f;
-        if (t < e1) {
-          at = a.tgt[t];
-          at = at < 0 || at >= a.v ? -1 : at - v0 - iw;
-          d = a.dlogp[t];
-        }
-        if (!__any(at >= 0 && at < 32 * S::FM)) continue;
+        for (int e = 0; e < 16; ++e) acc[f][g][e] = row.total != 0.f ? -row.total * fast_exp2(acc[f][g][e] * c - row.lse2) : 0.f;
+      // The targets among the wavefront's entries: few, so each is looked for in the registers.  place: where target e is.
+      auto place = [&](int e) {
+        const int t = e == row.e0 ? row.t0 : e < row.e1 ? a.tgt[e] : -1;
+        return t < 0 || t >= a.v ? -64 : t - v0 - iw - 4 * (lane >> 5);
+      };
+      auto here = [&](int at) { return at >= -4 && at < 32 * S::FM; };
+      for (int t = row.e0; __any(t < row.e1); ++t) {
+        const int at = place(t);
+        if (!__any(here(at))) continue;
+        const float d = t == row.e0 ? row.g0 : t < row.e1 ? a.dlogp[t] : 0.f;
 #pragma unroll
         for (int f = 0; f < S::FM; ++f)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (at == 32 * f + down(e, lane)) acc[f][g][e] += d;
+            if (at == 32 * f + down(e)) acc[f][g][e] += d;
       }
 #pragma unroll
       for (int f = 0; f < S::FM; ++f)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[f][g][e] = iw + 32 * f + down(e, lane) < W.rows ? acc[f][g][e] * a.scale : 0.f;
+        for (int e = 0; e < 16; ++e) acc[f][g][e] = 32 * f + down(e) < left ? acc[f][g][e] * a.scale : 0.f;
       if (PLANES == 1) {
         // A target's dz is most of its row's, so its rounding would be most of the gradients' error: what it leaves out
         // goes into them by itself.
-        for (int t = e0; __any(t < e1); ++t) {
-          int at = -1;
-          if (t < e1) {
-            const int v = a.tgt[t];
-            at = v < 0 || v >= a.v ? -1 : v - v0 - iw;
-            for (int u = e0; u < t; ++u)
-              if (a.tgt[u] == v) at = -1;
-          }
-          if (!__any(at >= 0 && at < 32 * S::FM)) continue;
+        for (int t = row.e0; __any(t < row.e1); ++t) {
+          int at = place(t);
+          if (!__any(here(at))) continue;
+          if (here(at))
+            for (int u = row.e0; u < t; ++u)
+              if (place(u) == at) at = -64;
           float x = 0.f;
           bool mine = false;
 #pragma unroll
           for (int f = 0; f < S::FM; ++f)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (at == 32 * f + down(e, lane)) x = acc[f][g][e], mine = true;
+              if (at == 32 * f + down(e)) x = acc[f][g][e], mine = true;
           if (mine) a.ent_rem[t] = is_finite(x) ? x - bf2f(pack2(x, 0.f) & 0xffffu) : 0.f;
         }
       }
@@ -566,13 +569,26 @@ __device__ __forceinline__ void put_rows(float* p, int i, int limit, const f32x1
     if (at < limit) *(f32x4*)(p + at) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
   }
 }
-// x += w times the same elements of a bf16 row
-__device__ __forceinline__ void add_rows(f32x16& x, float w, const bf16_t* p, int i, int limit, int lane) {
+// Segments of count rows of a bf16 matrix, elements i0 .. i0 + M - 1 (below limit) of row(k) for k < count, to LDS: rows of M
+// elements, chunk c of 16 bytes of row k at position c ^ (k mod M / 8).  row(k) < 0: left out.
+template <class S, class F>
+__device__ __forceinline__ void fetch_rows(F&& row, int count, const bf16_t* p, int64_t ld, int64_t i0, int limit, uint8_t* lds) {
+  constexpr int CH = S::M / 8;
+#pragma unroll 2
+  for (int x = threadIdx.x; x < count * CH; x += S::THREADS) {
+    const int k = x / CH, c = (x % CH) ^ (k % CH), r = row(k);
+    if (r >= 0 && i0 + 8 * c < limit) *(u32x4*)(lds + x * 16) = ld16(p + r * ld + i0 + 8 * c);
+  }
+}
+// x += w times row k there, elements i .. i + 31 of the tile (those below limit)
+template <class S>
+__device__ __forceinline__ void add_row(f32x16& x, float w, const uint8_t* lds, int k, int i, int limit, int lane) {
+  constexpr int CH = S::M / 8;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int at = i + 8 * q + 4 * (lane >> 5);
-    if (at >= limit) continue;
-    const u32x2 b = ld8(p + at);
+    const int c = i / 8 + q;
+    if (8 * c >= limit) continue;
+    const u32x2 b = ld8(lds + k * S::M * 2 + ((c ^ (k % CH)) << 4) + 8 * (lane >> 5));
     x[4 * q] = fmaf(w, bf2f(b[0] & 0xffffu), x[4 * q]);
     x[4 * q + 1] = fmaf(w, __uint_as_float(b[0] & 0xffff0000u), x[4 * q + 1]);
     x[4 * q + 2] = fmaf(w, bf2f(b[1] & 0xffffu), x[4 * q + 2]);
@@ -613,10 +629,27 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
   f32x16 acc[S::FM][S::FN];
+  const bool last = piece == a.pieces - 1, rest = PLANES == 1 && last && split == 0;   // rest: what the targets' dz left out is added
+  __shared__ struct { int32_t e0, e1; } s_row[PLANES == 1 ? S::N : 1];     // the rows' targets
+  __shared__ struct { float rem; int32_t t; } s_tgt[PLANES == 1 ? S::N : 1];   // and N at a time of those of all of them
+  int e_lo = 0, e_hi = 0;
+  auto list_targets = [&](int first) {
+    for (int j = threadIdx.x; j < S::N; j += S::THREADS) {
+      const float rem = first + j < e_hi ? a.ent_rem[first + j] : 0.f;
+      s_tgt[j] = {rem, rem != 0.f ? a.tgt[first + j] : -1};
+    }
+  };
+  if (rest) {
+    e_lo = a.row[j0].e0, e_hi = max(e_lo, a.row[min(j0 + S::N, (int64_t)a.n) - 1].e1);
+    for (int j = threadIdx.x; j < S::N; j += S::THREADS) {
+      s_row[j] = {0, 0};
+      if (j0 + j < a.n) s_row[j] = {max(a.row[j0 + j].e0, e_lo), min(a.row[j0 + j].e1, e_hi)};
+    }
+    list_targets(e_lo);
+  }
   const Operand W = part_of(swapped(w_operand(a, piece)), true, (int64_t)split * k, k);
   const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.np, a.piece_v}, false, (int64_t)split * k, k);
   product<S, PLANES, true, false>(acc, W, D, i0, j0, W.ks, lds);
-  const bool last = piece == a.pieces - 1;
   float* sums = a.dx_acc + (int64_t)split * a.n * a.h;
 #pragma unroll
   for (int g = 0; g < S::FN; ++g) {
@@ -634,18 +667,35 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
           for (int e = 0; e < 4; ++e) acc[f][g][4 * q + e] += y[e];
         }
     }
-    if (PLANES == 1 && last && split == 0) {   // what the targets' dz left out
-      int e0 = 0, e1 = 0;
-      if (limit) targets_of(a, (int)r, e0, e1);
-      for (int e = e0; e < e1; ++e) {
-        const float rem = a.ent_rem[e];
-        if (rem == 0.f) continue;
-        const bf16_t* w = (const bf16_t*)a.W + (int64_t)a.tgt[e] * a.h;
-#pragma unroll
-        for (int f = 0; f < S::FM; ++f) add_rows(acc[f][g], rem, w, iw + 32 * f, limit, lane);
+  }
+  if (rest) {
+    const int in = (int)min((int64_t)S::M, a.h - i0);   // elements of the tile
+    for (int first = e_lo; first < e_hi; first += S::N) {
+      if (first > e_lo) {
+        list_targets(first);
+        __syncthreads();
       }
+      fetch_rows<S>([&](int k) { return s_tgt[k].t; }, S::N, (const bf16_t*)a.W, a.h, i0, a.h, lds);
+      __syncthreads();
+#pragma unroll
+      for (int g = 0; g < S::FN; ++g) {
+        sched_fence();
+        const int j = jw + 32 * g + (lane & 31);
+        for (int e = max(s_row[j].e0, first); e < min(s_row[j].e1, first + S::N); ++e) {
+          const float rem = s_tgt[e - first].rem;
+          if (rem == 0.f) continue;
+#pragma unroll
+          for (int f = 0; f < S::FM; ++f) add_row<S>(acc[f][g], rem, lds, e - first, iw - (int)i0 + 32 * f, in, lane);
+        }
+      }
+      __syncthreads();
     }
-    if (!last || a.splits_dx > 1) {
+  }
+  if (!last || a.splits_dx > 1) {
+#pragma unroll
+    for (int g = 0; g < S::FN; ++g) {
+      const int64_t r = j0 + jw + 32 * g + (lane & 31);
+      const int limit = r < a.n ? a.h : 0;
 #pragma unroll
       for (int f = 0; f < S::FM; ++f) put_rows(sums + r * a.h, iw + 32 * f, limit, acc[f][g], lane);
     }
@@ -663,43 +713,92 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
   f32x16 acc[S::FM][S::FN];
+  const int v0 = piece * a.piece_v + (int)j0, vn = min(S::N, min(a.piece_v - (int)j0, a.v - v0));   // the tile's entries
+  // What the targets' dz left out (rest): the targets are looked through for this tile's entries, 64 per wavefront and turn,
+  // and those found are listed in their order, as many at a time as the list holds in any case.
+  constexpr int TURNS = 8, LIST = PLANES == 1 ? 256 * S::WAVES : 1;
+  __shared__ struct { float rem; int32_t row, col; } s_list[LIST];
+  __shared__ int s_count[S::WAVES];
+  const bool rest = PLANES == 1 && split == 0;
+  int listed = 0, seen = 0, taken = 0;   // of the batch from seen on, `taken` have been listed before
+  auto collect = [&] {
+    listed = 0;
+    while (seen < a.e && listed < LIST) {
+      uint64_t mask[TURNS];
+      int t[TURNS], mine = 0;
+#pragma unroll
+      for (int u = 0; u < TURNS; ++u) {
+        const int e = seen + (wave * TURNS + u) * 64 + lane;
+        t[u] = e < a.e ? a.tgt[e] - v0 : -1;
+      }
+#pragma unroll
+      for (int u = 0; u < TURNS; ++u) {
+        mask[u] = __ballot(t[u] >= 0 && t[u] < vn);
+        mine += __builtin_popcountll(mask[u]);
+      }
+      __syncthreads();
+      if (lane == 0) s_count[wave] = mine;
+      __syncthreads();
+      int at = listed - taken, all = -taken;
+#pragma unroll
+      for (int w = 0; w < S::WAVES; ++w) {
+        const int n = s_count[w];
+        if (w < wave) at += n;
+        all += n;
+      }
+#pragma unroll
+      for (int u = 0; u < TURNS; ++u) {
+        const int k = at + __builtin_popcountll(mask[u] & ((1ull << lane) - 1));
+        if ((mask[u] >> lane & 1) && k >= listed && k < LIST) s_list[k] = {0.f, seen + (wave * TURNS + u) * 64 + lane, t[u]};
+        at += __builtin_popcountll(mask[u]);
+      }
+      if (listed + all > LIST) {
+        taken += LIST - listed;
+        listed = LIST;
+        break;
+      }
+      listed += all;
+      taken = 0;
+      seen += 64 * TURNS * S::WAVES;
+    }
+    __syncthreads();
+    for (int k = threadIdx.x; k < listed; k += S::THREADS) {
+      const int e = s_list[k].row, r = a.ent_row[e];
+      int e0 = 0, e1 = 0;
+      if (r >= 0 && r < a.n) targets_of(a, r, e0, e1);   // (a target that no row lists has no row here)
+      const float rem = e >= e0 && e < e1 ? a.ent_rem[e] : 0.f;
+      s_list[k].rem = rem;
+      s_list[k].row = rem != 0.f ? r : -1;
+    }
+  };
+  if (rest) collect();
   const Operand X = part_of({a.xc, a.hp, (int64_t)a.np * a.hp, a.hp, a.np}, true, (int64_t)split * k, k);
   const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, a.np}, true, (int64_t)split * k, k);
   product<S, PLANES, true, true>(acc, X, D, i0, j0, X.ks, lds);
-  const int v0 = piece * a.piece_v + (int)j0, vn = min(S::N, min(a.piece_v - (int)j0, a.v - v0));   // the tile's entries
-  if (PLANES == 1 && split == 0) {
-    // What the targets' dz left out: the targets are looked through for this tile's entries, 64 per wavefront and turn, and
-    // taken in their order.
-    constexpr int TURNS = 8, WORDS = TURNS * S::WAVES;
-    uint64_t* found = (uint64_t*)lds;
-    for (int base = 0; base < a.e; base += 64 * WORDS) {
-      if (base) __syncthreads();
-#pragma unroll
-      for (int u = 0; u < TURNS; ++u) {
-        const int e = base + (wave * TURNS + u) * 64 + lane, t = e < a.e ? a.tgt[e] : -1;
-        const uint64_t mask = __ballot(t >= v0 && t < v0 + vn);
-        if (lane == 0) found[wave * TURNS + u] = mask;
-      }
+  if (rest) {
+    const int in = (int)min((int64_t)S::M, a.h - i0);
+    for (;;) {
       __syncthreads();
-      for (int w = 0; w < WORDS && base + 64 * w < a.e; ++w) {
-        for (uint64_t mask = found[w]; mask; mask &= mask - 1) {
-          const int e = base + 64 * w + __builtin_ctzll(mask), j = a.tgt[e] - v0 - jw, r = a.ent_row[e];
-          // (a target that no row lists has no row here)
-          if (j < 0 || j >= 32 * S::FN || r < 0 || r >= a.n) continue;
-          int e0, e1;
-          targets_of(a, r, e0, e1);
-          const float rem = e >= e0 && e < e1 ? a.ent_rem[e] : 0.f;
-          if (rem == 0.f) continue;
+      for (int c = 0; c < listed; c += S::N) {
+        const int n = min(S::N, listed - c);
+        fetch_rows<S>([&](int k) { return s_list[c + k].row; }, n, a.xc, a.hp, i0, a.h, lds);
+        __syncthreads();
+        for (int k = 0; k < n; ++k) {
+          const int j = s_list[c + k].col - jw;
+          const float rem = s_list[c + k].rem;
+          if (j < 0 || j >= 32 * S::FN || rem == 0.f) continue;
 #pragma unroll
           for (int g = 0; g < S::FN; ++g)
             if (j == 32 * g + (lane & 31)) {
 #pragma unroll
-              for (int f = 0; f < S::FM; ++f) add_rows(acc[f][g], rem, a.xc + (int64_t)r * a.hp, iw + 32 * f, a.h, lane);
+              for (int f = 0; f < S::FM; ++f) add_row<S>(acc[f][g], rem, lds, k, iw - (int)i0 + 32 * f, in, lane);
             }
         }
+        __syncthreads();
       }
+      if (seen >= a.e) break;
+      collect();
     }
-    __syncthreads();
   }
   if (a.splits_dw > 1) {
     float* sums = a.dw_acc + (int64_t)split * a.piece_v * a.h;

@@ -123,7 +123,7 @@ __device__ __forceinline__ void step_chunk(const AdamwTensor& t, P* weights, con
   PSATTN_NO_CONTRACT
   const float keep = (float)(1.0 - s.lr_decay * (double)t.decay);
   const int64_t end = min(t.n, base + ADAMW_CHUNK);
-#pragma unroll 2
+#pragma unroll 1
   for (int64_t at = base; at < end; at += TURN) {
     const int64_t i = at + 4 * tid;
     const int n = (int)min((int64_t)4, end - i);   // (0 or less: nothing, but the lane takes part in its block)
@@ -146,7 +146,7 @@ __device__ __forceinline__ void step_chunk(const AdamwTensor& t, P* weights, con
       const float g = gr[k] * s.gs;
       m[k] = m[k] * s.b1 + g * s.ob1;
       v[k] = v[k] * s.b2 + (g * g) * s.ob2;
-      r[k] = __fsqrt_rn(v[k]);
+      r[k] = sqrtf(v[k]);
       w[k] = w[k] * keep - (m[k] / (r[k] * s.inv_sb2 + s.eps)) * s.lr_t;
     }
     store4(weights, i, n, w);
@@ -231,6 +231,7 @@ __global__ __launch_bounds__(1024) void adamw_scalars_kernel(AdamwArgs a, int wi
   PSATTN_NO_CONTRACT
   double x = 0;
   if (with_norm)
+#pragma unroll 8
     for (int i = threadIdx.x; i < a.total_items; i += 1024) x += a.part[i];
   x = block_sum<1024>(x);
   if (threadIdx.x) return;

@@ -104,16 +104,13 @@ struct Reader {
       for (int kk = 0; kk < BK / 16; ++kk) at[kk] = r * BK * 2 + (((2 * kk + (lane >> 5)) ^ kswz<BK>(r)) << 4);
     }
   }
-  template <int KK>
-  __device__ __forceinline__ void read(bf16x8 (&x)[FRAGS], const uint8_t* tile) const {
-#pragma unroll
-    for (int f = 0; f < FRAGS; ++f) {
-      if constexpr (KOUTER) {
-        const uint8_t* p = tile + at[f] + KK * 16 * I * 2;
-        x[f] = as_bf(lds_tr(p), lds_tr(p + 4 * I * 2));
-      } else {
-        x[f] = as_bf(ld16(tile + at[KK] + f * 32 * BK * 2));
-      }
+  template <int KK, int F>
+  __device__ __forceinline__ bf16x8 read(const uint8_t* tile) const {
+    if constexpr (KOUTER) {
+      const uint8_t* p = tile + at[F] + KK * 16 * I * 2;
+      return as_bf(lds_tr(p), lds_tr(p + 4 * I * 2));
+    } else {
+      return as_bf(ld16(tile + at[KK] + F * 32 * BK * 2));
     }
   }
 };
@@ -195,40 +192,47 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
   for (int s = 0; s < S::RING - 1 && s < steps; ++s) issue();
   landed(S::RING - 1 <= steps);
   if (S::RING - 1 < steps) issue();
-  ra.template read<0>(fa[0], lds);
-  rb.template read<0>(fb[0], lds + S::M * BK * 2);
+  // fragment F of the operands' FM + FN, elements 16 KK .. of a stage
+  auto read = [&](auto kk, auto frag, const uint8_t* tile) {
+    constexpr int KK = decltype(kk)::value, F = decltype(frag)::value;
+    if constexpr (F < S::FM) fa[KK & 1][F] = ra.template read<KK, F>(tile);
+    else fb[KK & 1][F - S::FM] = rb.template read<KK, F - S::FM>(tile + S::M * BK * 2);
+  };
+  static_for<S::FM + S::FN>([&](auto f) { read(IntC<0>{}, f, lds); });
   int use = 0;
-  // One stage: COPY: a later stage is copied meanwhile, into this one's place; NEXT: a stage follows.
+  // One stage: COPY: a later stage is copied meanwhile, into this one's place; NEXT: a stage follows.  Between two products of
+  // a wavefront stands one read of the operands of the products behind this quarter, or a copy.
   auto stage = [&](auto copy_flag, auto next_flag) {
     constexpr bool COPY = decltype(copy_flag)::value, NEXT = decltype(next_flag)::value;
+    constexpr int PRODUCTS = S::FM * S::FN, READS = S::FM + S::FN;
     const uint8_t* tile = lds + use * S::STAGE;
     if (++use == S::RING) use = 0;
     const uint8_t* next = lds + use * S::STAGE;
     static_for<QS>([&](auto q) {
       constexpr int KK = decltype(q)::value;
-      if constexpr (KK < QS - 1) {
-        ra.template read<(KK + 1) % QS>(fa[(KK + 1) & 1], tile);
-        rb.template read<(KK + 1) % QS>(fb[(KK + 1) & 1], tile + S::M * BK * 2);
-      } else if constexpr (NEXT) {
+      constexpr bool LAST = KK == QS - 1;
+      constexpr int ACTIONS = (LAST && !NEXT ? 0 : READS) + (LAST && COPY ? COPIES : 0);
+      constexpr int PER = (ACTIONS + PRODUCTS - 1) / PRODUCTS;
+      if constexpr (LAST && NEXT) {
         wait_lds<0>();
         landed(COPY);
-        ra.template read<0>(fa[0], next);
-        rb.template read<0>(fb[0], next + S::M * BK * 2);
         if constexpr (COPY) point();
       }
-      sched_fence();   // (the reads stay ahead of the products of what was read before, and the copies among these)
-      static_for<S::FM * S::FN>([&](auto m) {
-        constexpr int I = decltype(m)::value, F = I / S::FN, G = I % S::FN, PER = (COPIES + S::FM * S::FN - 1) / (S::FM * S::FN);
-        acc[F][G] = mfma(fa[KK & 1][F], fb[KK & 1][G], acc[F][G]);
-        if constexpr (COPY && KK == QS - 1) {
-          sched_fence();
-          static_for<PER>([&](auto j) {
-            if constexpr (I * PER + decltype(j)::value < COPIES) copy(IntC<I * PER + decltype(j)::value>{});
-          });
-          sched_fence();
-        }
-      });
       sched_fence();
+      static_for<PRODUCTS>([&](auto m) {
+        constexpr int I = decltype(m)::value, F = I / S::FN, G = I % S::FN;
+        acc[F][G] = mfma(fa[KK & 1][F], fb[KK & 1][G], acc[F][G]);
+        sched_fence();
+        static_for<PER>([&](auto j) {
+          constexpr int A = I * PER + decltype(j)::value;
+          if constexpr (A < ACTIONS) {
+            if constexpr (A >= READS) copy(IntC<A - READS>{});
+            else if constexpr (LAST) read(IntC<0>{}, IntC<A>{}, next);
+            else read(IntC<(KK + 1) % QS>{}, IntC<A>{}, tile);
+          }
+        });
+        sched_fence();
+      });
     });
   };
   int s = 0;
@@ -392,23 +396,27 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
   const int left = W.rows - iw - 4 * (lane >> 5);   // element (f, e) is an entry where 32 f + down(e) is below
   if constexpr (!BACKWARD) {
     LogprobStat* part = (LogprobStat*)lds;                 // [WM][N]
+    if (left < 32 * S::FM) {
+#pragma unroll
+      for (int g = 0; g < S::FN; ++g)
+#pragma unroll
+        for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[f][g][e] = 32 * f + down(e) < left ? acc[f][g][e] : kNegInf;
+    }
 #pragma unroll
     for (int g = 0; g < S::FN; ++g) {
       float top = kNegInf, sum = 0.f;
 #pragma unroll
       for (int f = 0; f < S::FM; ++f)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const bool in = 32 * f + down(e) < left;
-          acc[f][g][e] = in ? acc[f][g][e] * c : kNegInf;
-          top = fmaxf(top, acc[f][g][e]);
-        }
-      top = pair_max(top);
+        for (int e = 0; e < 16; e += 2) top = max3f(top, acc[f][g][e], acc[f][g][e + 1]);
+      top = pair_max(top) * c;                             // (c > 0)
       const float ref = top == kNegInf ? 0.f : top;
 #pragma unroll
       for (int f = 0; f < S::FM; ++f)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sum += fast_exp2(acc[f][g][e] - ref);
+        for (int e = 0; e < 16; ++e) sum += fast_exp2(fmaf(acc[f][g][e], c, -ref));
       sum = pair_sum(sum);
       if (lane < 32) part[wave / S::WN * S::N + jw + 32 * g + lane] = {top, sum};
     }
@@ -427,10 +435,12 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
       sched_fence();
       LogprobRow row = {0.f, 0.f, 0.f, -1, 0, 0, {0, 0}};
       if (j0 + jw + 32 * g < a.np) row = s_row[jw + 32 * g + (lane & 31)];
+      // (a row whose G is 0 takes 2^-inf: nothing, whatever its LSE)
+      const float k = -row.total * a.scale, ref = k == 0.f ? -kNegInf : row.lse2;
 #pragma unroll
       for (int f = 0; f < S::FM; ++f)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[f][g][e] = row.total != 0.f ? -row.total * fast_exp2(acc[f][g][e] * c - row.lse2) : 0.f;
+        for (int e = 0; e < 16; ++e) acc[f][g][e] = k * fast_exp2(fmaf(acc[f][g][e], c, -ref));
       // The targets among the wavefront's entries: few, so each is looked for in the registers.  place: where target e is.
       auto place = [&](int e) {
         const int t = e == row.e0 ? row.t0 : e < row.e1 ? a.tgt[e] : -1;
@@ -440,17 +450,19 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
       for (int t = row.e0; __any(t < row.e1); ++t) {
         const int at = place(t);
         if (!__any(here(at))) continue;
-        const float d = t == row.e0 ? row.g0 : t < row.e1 ? a.dlogp[t] : 0.f;
+        const float d = a.scale * (t == row.e0 ? row.g0 : t < row.e1 ? a.dlogp[t] : 0.f);
 #pragma unroll
         for (int f = 0; f < S::FM; ++f)
 #pragma unroll
           for (int e = 0; e < 16; ++e)
             if (at == 32 * f + down(e)) acc[f][g][e] += d;
       }
+      if (left < 32 * S::FM) {
 #pragma unroll
-      for (int f = 0; f < S::FM; ++f)
+        for (int f = 0; f < S::FM; ++f)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[f][g][e] = 32 * f + down(e) < left ? acc[f][g][e] * a.scale : 0.f;
+          for (int e = 0; e < 16; ++e) acc[f][g][e] = 32 * f + down(e) < left ? acc[f][g][e] : 0.f;
+      }
       if (PLANES == 1) {
         // A target's dz is most of its row's, so its rounding would be most of the gradients' error: what it leaves out
         // goes into them by itself.

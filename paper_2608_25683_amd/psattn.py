@@ -15,6 +15,7 @@ Names follow the C ABI in include/psattn.h:
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Optional, Sequence, Tuple
 
@@ -693,6 +694,9 @@ def psattn_logprob_bwd(X, W, tgt_ptr, tgt, LSE, dlogp, logit_scale: float = 1.0,
     return dX, dW
 
 
+_dtype_of = operator.attrgetter("dtype")
+
+
 class AdamW:
     """AdamW over a list of weights (psattn_adamw_*): fp32 tensors, or bf16 ones with fp32 masters, updated in place.
 
@@ -776,8 +780,7 @@ class AdamW:
         _check(L.psattn_adamw_workspace_size(h, ctypes.byref(size)))
         self._ws_bytes = size.value
         self._sizes = [p.numel() for p in self.params]
-        self._pointers = ctypes.c_void_p * n
-        self._dtypes = ctypes.c_int32 * n
+        self._index = self.params[0].get_device()
 
     def __del__(self):
         if getattr(self, "_handle", None) is not None and _LIB is not None:
@@ -791,12 +794,26 @@ class AdamW:
         where that is not finite); the norm before clipping is then returned (fp32 [1]), else None.  ``dyn`` (int32 [4] on
         the GPU, see :meth:`dyn`): lr, grad_scale, step and seed are read from it instead, also by replays of a captured step."""
         import torch
-        if len(grads) != len(self.params):
-            raise ValueError(f"{len(grads)} gradients for {len(self.params)} weights")
-        f32, bf16, device = torch.float32, torch.bfloat16, self.device
-        for i, (g, n) in enumerate(zip(grads, self._sizes)):
-            if g is not None and (g.numel() != n or (g.dtype is not f32 and g.dtype is not bf16) or g.device != device or not g.is_contiguous()):
-                raise ValueError(f"grads[{i}]: expected {n} contiguous bf16 or fp32 elements on {device}, got {g.dtype} {tuple(g.shape)} on {g.device}")
+        T, f32, device = torch.Tensor, torch.float32, self.device
+        n = len(self.params)
+        if len(grads) != n:
+            raise ValueError(f"{len(grads)} gradients for {n} weights")
+        given = [g for g in grads if g is not None]
+        kinds = set(map(_dtype_of, given))
+        # (whole lists at a time: a step over hundreds of small tensors is bound by these checks)
+        if not (list(map(T.numel, given)) == [k for k, g in zip(self._sizes, grads) if g is not None] and all(map(T.is_contiguous, given))
+                and kinds <= {f32, torch.bfloat16} and set(map(T.get_device, given)) <= {self._index}):
+            for i, (g, k) in enumerate(zip(grads, self._sizes)):
+                if g is not None and (g.numel() != k or g.dtype not in (f32, torch.bfloat16) or g.device != device or not g.is_contiguous()):
+                    raise ValueError(f"grads[{i}]: expected {k} contiguous bf16 or fp32 elements on {device}, got {g.dtype} {tuple(g.shape)} on {g.device}")
+        if len(given) == n:
+            pointers = np.fromiter(map(T.data_ptr, grads), np.uint64, n)
+        else:
+            pointers = np.array([0 if g is None else g.data_ptr() for g in grads], np.uint64)
+        if len(kinds) == 1:
+            dtypes = np.full(n, PSATTN_FP32 if f32 in kinds else PSATTN_BF16, np.int32)
+        else:
+            dtypes = np.array([PSATTN_FP32 if g is None or g.dtype is f32 else PSATTN_BF16 for g in grads], np.int32)
         if dyn is not None:
             _need(dyn, (4,), torch.int32, "dyn")
             _same_device(self.params[0], (dyn, "dyn"))
@@ -804,9 +821,7 @@ class AdamW:
         ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=device)
         hyper = AdamwHyper(lr, betas[0], betas[1], eps, weight_decay, max_norm, grad_scale, step, seed & 0xffffffff, 0)
         with torch.cuda.device(device):
-            _check(lib().psattn_adamw_step(self._handle, self._pointers(*[0 if g is None else g.data_ptr() for g in grads]),
-                                           self._dtypes(*[PSATTN_BF16 if g is not None and g.dtype is bf16 else PSATTN_FP32 for g in grads]),
-                                           ctypes.byref(hyper), _vp(dyn), _vp(norm), _vp(ws), self._ws_bytes,
+            _check(lib().psattn_adamw_step(self._handle, _ptr(pointers, ctypes.c_void_p), _ptr(dtypes, ctypes.c_int32), ctypes.byref(hyper), _vp(dyn), _vp(norm), _vp(ws), self._ws_bytes,
                                            ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)))
         return norm
 

@@ -1403,7 +1403,7 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   a.piece_v = (int32_t)(256 * each);
   if ((int64_t)(a.n / 32 + 1) * (std::max(a.v, a.h) / 128 + 1) > INT32_MAX / 32)
     return fail(PSATTN_E_UNSUPPORTED, "rows %d x vocab %d: more tiles than a launch holds", a.n, a.v);
-  a.shape = !bwd && a.n <= 32 ? LP_THIN : logprob_tiling(std::min(a.v, a.piece_v), a.n, a.hp, a.planes, 1).shape;
+  a.shape = a.n <= 32 ? LP_THIN : logprob_tiling(std::min(a.v, a.piece_v), a.n, a.hp, a.planes, 1).shape;
   a.part_v = a.shape == LP_LARGE ? 256 : 128;
   const LogprobTiling dx = logprob_tiling(a.h, a.n, std::min(a.v, a.piece_v), a.planes, 32);
   const LogprobTiling dw = logprob_tiling(a.h, std::min(a.v, a.piece_v), a.n, a.planes, 32);

@@ -26,7 +26,7 @@ struct Shape2 {
 using Large = Shape2<2, 4, 4, 2, 64, 2>;    // 256 x 256, one workgroup per CU
 using Small = Shape2<2, 2, 2, 2, 64, 2>;    // 128 x 128, two
 using Deep = Shape2<2, 2, 2, 2, 64, 4>;     // 128 x 128, one, three stages ahead
-using Thin = Shape2<4, 1, 1, 1, 64, 2>;     // 128 x 32, four
+using Thin = Shape2<4, 1, 1, 1, 64, 6>;     // 128 x 32, one: 100 KB of copies on their way
 
 // An operand of a product: element (i, k) of plane q at p + q plane + i ld + k, or + k ld + i where K is the outer dimension.
 // Reads of i >= rows and k >= ks give some element of the operand in their place: such i are not stored, and at
@@ -581,31 +581,56 @@ __device__ __forceinline__ void put_rows(float* p, int i, int limit, const f32x1
     if (at < limit) *(f32x4*)(p + at) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
   }
 }
-// Segments of count rows of a bf16 matrix, elements i0 .. i0 + M - 1 (below limit) of row(k) for k < count, to LDS: rows of M
-// elements, chunk c of 16 bytes of row k at position c ^ (k mod M / 8).  row(k) < 0: left out.
+// One of the terms rem(k) row(k) (down) at column col(k) (across) that are added to a tile; no row: nothing.
+struct Term { const bf16_t* row; int32_t col; float rem; };
+// acc += the terms, as products like any other: 64 at a time are a stage whose B is rem (as bf16, which leaves 2^-9 of what is
+// itself below 2^-9 of the term it belongs to) at the term's column and zero elsewhere.  Elements i0 .. of the rows
+// (below limit) go down the tile.
 template <class S, class F>
-__device__ __forceinline__ void fetch_rows(F&& row, int count, const bf16_t* p, int64_t ld, int64_t i0, int limit, uint8_t* lds) {
-  constexpr int CH = S::M / 8;
+__device__ __forceinline__ void add_terms(f32x16 (&acc)[S::FM][S::FN], int count, F&& term, int64_t i0, int limit, uint8_t* lds) {
+  constexpr int CM = S::M / 8, CN = S::N / 8;
+  static_assert((S::M + S::N) * 128 <= S::LDS, "a stage of 64 fits");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint8_t* b = lds + S::M * 128;
+  const Reader<S::M, 64, S::FM, true> ra(wave / S::WN * S::FM * 32, lane);
+  const Reader<S::N, 64, S::FN, true> rb(wave % S::WN * S::FN * 32, lane);
+#pragma unroll 1
+  for (int first = 0; first < count; first += 64) {
+    __syncthreads();
 #pragma unroll 2
-  for (int x = threadIdx.x; x < count * CH; x += S::THREADS) {
-    const int k = x / CH, c = (x % CH) ^ (k % CH), r = row(k);
-    if (r >= 0 && i0 + 8 * c < limit) *(u32x4*)(lds + x * 16) = ld16(p + r * ld + i0 + 8 * c);
-  }
-}
-// x += w times row k there, elements i .. i + 31 of the tile (those below limit)
-template <class S>
-__device__ __forceinline__ void add_row(f32x16& x, float w, const uint8_t* lds, int k, int i, int limit, int lane) {
-  constexpr int CH = S::M / 8;
+    for (int x = threadIdx.x; x < 64 * CM; x += S::THREADS) {
+      const int k = x / CM, c = (x % CM) ^ ((k & 3) << 2);
+      const bf16_t* row = first + k < count ? term(first + k).row : nullptr;
+      u32x4 y = {0, 0, 0, 0};
+      if (row && i0 + 8 * c < limit) y = ld16(row + i0 + 8 * c);
+      *(u32x4*)(lds + x * 16) = y;
+    }
+    for (int x = threadIdx.x; x < 64 * CN; x += S::THREADS) *(u32x4*)(b + x * 16) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+    if (threadIdx.x < 64 && first + (int)threadIdx.x < count) {
+      const int k = threadIdx.x;
+      const Term t = term(first + k);
+      if (t.row) *(bf16_t*)(b + k * S::N * 2 + (((t.col >> 3) ^ ((k & 3) << 2)) << 4) + (t.col & 7) * 2) = (bf16_t)pack2(t.rem, 0.f);
+    }
+    __syncthreads();
+    static_for<4>([&](auto q) {
+      constexpr int KK = decltype(q)::value;
+      bf16x8 fa[S::FM], fb[S::FN];
+      static_for<S::FM>([&](auto f) { fa[decltype(f)::value] = ra.template read<KK, decltype(f)::value>(lds); });
+      static_for<S::FN>([&](auto f) { fb[decltype(f)::value] = rb.template read<KK, decltype(f)::value>(b); });
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int c = i / 8 + q;
-    if (8 * c >= limit) continue;
-    const u32x2 b = ld8(lds + k * S::M * 2 + ((c ^ (k % CH)) << 4) + 8 * (lane >> 5));
-    x[4 * q] = fmaf(w, bf2f(b[0] & 0xffffu), x[4 * q]);
-    x[4 * q + 1] = fmaf(w, __uint_as_float(b[0] & 0xffff0000u), x[4 * q + 1]);
-    x[4 * q + 2] = fmaf(w, bf2f(b[1] & 0xffffu), x[4 * q + 2]);
-    x[4 * q + 3] = fmaf(w, __uint_as_float(b[1] & 0xffff0000u), x[4 * q + 3]);
+      for (int f = 0; f < S::FM; ++f)
+#pragma unroll
+        for (int g = 0; g < S::FN; ++g) acc[f][g] = mfma(fa[f], fb[g], acc[f][g]);
+    });
   }
+  __syncthreads();
+}
+// Target e as a term of its row r: what the rounding of its dz left out, 0 if row r does not list it.
+__device__ __forceinline__ float rem_of(const LogprobArgs& a, int e, int r) {
+  int e0 = 0, e1 = 0;
+  if (r >= 0 && r < a.n) targets_of(a, r, e0, e1);
+  return e >= e0 && e < e1 ? a.ent_rem[e] : 0.f;
 }
 // the workgroup's tile to a result of the inputs' type
 template <class S, int PLANES>
@@ -642,22 +667,20 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
   f32x16 acc[S::FM][S::FN];
   const bool last = piece == a.pieces - 1, rest = PLANES == 1 && last && split == 0;   // rest: what the targets' dz left out is added
-  __shared__ struct { int32_t e0, e1; } s_row[PLANES == 1 ? S::N : 1];     // the rows' targets
-  __shared__ struct { float rem; int32_t t; } s_tgt[PLANES == 1 ? S::N : 1];   // and N at a time of those of all of them
+  // (the tile's rows have their targets one behind the other: LIST at a time, the first ones ahead of the products)
+  constexpr int LIST = PLANES == 1 ? 2 * S::N : 1;
+  __shared__ struct { float rem; int32_t tgt, col; } s_list[LIST];
   int e_lo = 0, e_hi = 0;
-  auto list_targets = [&](int first) {
-    for (int j = threadIdx.x; j < S::N; j += S::THREADS) {
-      const float rem = first + j < e_hi ? a.ent_rem[first + j] : 0.f;
-      s_tgt[j] = {rem, rem != 0.f ? a.tgt[first + j] : -1};
+  auto list = [&] {
+    for (int k = threadIdx.x; k < LIST && e_lo + k < e_hi; k += S::THREADS) {
+      const int e = e_lo + k, r = a.ent_row[e], t = a.tgt[e];
+      const bool in = r >= j0 && r < min(j0 + S::N, (int64_t)a.n) && t >= 0 && t < a.v;
+      s_list[k] = {in ? rem_of(a, e, r) : 0.f, t, (int)(r - j0)};
     }
   };
   if (rest) {
     e_lo = a.row[j0].e0, e_hi = max(e_lo, a.row[min(j0 + S::N, (int64_t)a.n) - 1].e1);
-    for (int j = threadIdx.x; j < S::N; j += S::THREADS) {
-      s_row[j] = {0, 0};
-      if (j0 + j < a.n) s_row[j] = {max(a.row[j0 + j].e0, e_lo), min(a.row[j0 + j].e1, e_hi)};
-    }
-    list_targets(e_lo);
+    list();
   }
   const Operand W = part_of(swapped(w_operand(a, piece)), true, (int64_t)split * k, k);
   const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.np, a.piece_v}, false, (int64_t)split * k, k);
@@ -681,26 +704,12 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
     }
   }
   if (rest) {
-    const int in = (int)min((int64_t)S::M, a.h - i0);   // elements of the tile
-    for (int first = e_lo; first < e_hi; first += S::N) {
-      if (first > e_lo) {
-        list_targets(first);
-        __syncthreads();
-      }
-      fetch_rows<S>([&](int k) { return s_tgt[k].t; }, S::N, (const bf16_t*)a.W, a.h, i0, a.h, lds);
-      __syncthreads();
-#pragma unroll
-      for (int g = 0; g < S::FN; ++g) {
-        sched_fence();
-        const int j = jw + 32 * g + (lane & 31);
-        for (int e = max(s_row[j].e0, first); e < min(s_row[j].e1, first + S::N); ++e) {
-          const float rem = s_tgt[e - first].rem;
-          if (rem == 0.f) continue;
-#pragma unroll
-          for (int f = 0; f < S::FM; ++f) add_row<S>(acc[f][g], rem, lds, e - first, iw - (int)i0 + 32 * f, in, lane);
-        }
-      }
-      __syncthreads();
+    while (e_lo < e_hi) {
+      add_terms<S>(
+          acc, min(LIST, e_hi - e_lo),
+          [&](int k) { return Term{s_list[k].rem != 0.f ? (const bf16_t*)a.W + (int64_t)s_list[k].tgt * a.h : nullptr, s_list[k].col, s_list[k].rem}; }, i0, a.h, lds);
+      e_lo += LIST;
+      list();
     }
   }
   if (!last || a.splits_dx > 1) {
@@ -776,11 +785,8 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
     __syncthreads();
     for (int k = threadIdx.x; k < listed; k += S::THREADS) {
       const int e = s_list[k].row, r = a.ent_row[e];
-      int e0 = 0, e1 = 0;
-      if (r >= 0 && r < a.n) targets_of(a, r, e0, e1);   // (a target that no row lists has no row here)
-      const float rem = e >= e0 && e < e1 ? a.ent_rem[e] : 0.f;
-      s_list[k].rem = rem;
-      s_list[k].row = rem != 0.f ? r : -1;
+      s_list[k].rem = rem_of(a, e, r);
+      s_list[k].row = r;
     }
   };
   if (rest) collect();
@@ -788,26 +794,10 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
   const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, a.np}, true, (int64_t)split * k, k);
   product<S, PLANES, true, true>(acc, X, D, i0, j0, X.ks, lds);
   if (rest) {
-    const int in = (int)min((int64_t)S::M, a.h - i0);
     for (;;) {
-      __syncthreads();
-      for (int c = 0; c < listed; c += S::N) {
-        const int n = min(S::N, listed - c);
-        fetch_rows<S>([&](int k) { return s_list[c + k].row; }, n, a.xc, a.hp, i0, a.h, lds);
-        __syncthreads();
-        for (int k = 0; k < n; ++k) {
-          const int j = s_list[c + k].col - jw;
-          const float rem = s_list[c + k].rem;
-          if (j < 0 || j >= 32 * S::FN || rem == 0.f) continue;
-#pragma unroll
-          for (int g = 0; g < S::FN; ++g)
-            if (j == 32 * g + (lane & 31)) {
-#pragma unroll
-              for (int f = 0; f < S::FM; ++f) add_row<S>(acc[f][g], rem, lds, k, iw - (int)i0 + 32 * f, in, lane);
-            }
-        }
-        __syncthreads();
-      }
+      add_terms<S>(
+          acc, listed,
+          [&](int k) { return Term{s_list[k].rem != 0.f ? a.xc + (int64_t)s_list[k].row * a.hp : nullptr, s_list[k].col, s_list[k].rem}; }, i0, a.h, lds);
       if (seen >= a.e) break;
       collect();
     }
@@ -863,8 +853,8 @@ void logits(const LogprobArgs& a, int piece, hipStream_t st) {
   const int rows = piece_rows(a, piece), n = BACKWARD ? a.np : a.n;
   if (a.shape == LP_LARGE) launch_tiles<Large>(logits_kernel<Large, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
   else if (a.shape == LP_SMALL) launch_tiles<Small>(logits_kernel<Small, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
-  else if (BACKWARD || a.shape == LP_DEEP) launch_tiles<Deep>(logits_kernel<Deep, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
-  else launch_tiles<Thin>(logits_kernel<Thin, PLANES, false>, rows, n, 1, a, piece, st);
+  else if (a.shape == LP_DEEP) launch_tiles<Deep>(logits_kernel<Deep, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
+  else launch_tiles<Thin>(logits_kernel<Thin, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
 }
 template <int PLANES>
 void dx(const LogprobArgs& a, int piece, hipStream_t st) {

@@ -15,6 +15,7 @@ Names follow the C ABI in include/psattn.h:
 from __future__ import annotations
 
 import ctypes
+import functools
 import operator
 import os
 from typing import Optional, Sequence, Tuple
@@ -201,7 +202,7 @@ def lib() -> ctypes.CDLL:
         L.psattn_adamw_device_bytes.argtypes = [vp, ctypes.POINTER(sz)]
         L.psattn_adamw_upload.argtypes = [vp, vp, sz, vp]
         L.psattn_adamw_workspace_size.argtypes = [vp, ctypes.POINTER(sz)]
-        L.psattn_adamw_step.argtypes = [vp, ctypes.POINTER(vp), _i32p, ctypes.POINTER(AdamwHyper), vp, vp, vp, sz, vp]
+        L.psattn_adamw_step.argtypes = [vp, vp, vp, ctypes.POINTER(AdamwHyper), vp, vp, vp, sz, vp]
         L.psattn_adamw_destroy.restype = None
         for name in EXPORTED:
             if name not in ("psattn_tree_destroy", "psattn_status_string", "psattn_last_error", "psattn_adamw_destroy"):
@@ -613,40 +614,60 @@ def _same_device(x, *others):
             raise ValueError(f"{name} is on {t.device}, not on {x.device}")
 
 
+def _expect(t, shape, dtype, index, name):
+    """_need and _same_device in one, for calls whose smallest ones take as long as their checks."""
+    if getattr(t, "shape", None) != shape or t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        _need(t, shape, dtype, name)
+        raise ValueError(f"{name} is on {t.device}, not on GPU {index}")
+
+
+def _on(index, call, *args):
+    """call(*args, stream) on the current stream of GPU `index`, with that GPU current."""
+    import torch
+    stream = ctypes.c_void_p(torch.cuda.current_stream(index).cuda_stream)
+    if torch.cuda.current_device() == index:
+        _check(call(*args, stream))
+    else:
+        with torch.cuda.device(index):
+            _check(call(*args, stream))
+
+
 def _logprob_args(X, W, tgt_ptr, tgt, logit_scale):
     import torch
-    if not isinstance(X, torch.Tensor) or not isinstance(W, torch.Tensor):
-        raise TypeError("X and W must be torch tensors")
-    if X.dtype not in (torch.bfloat16, torch.float32):
+    if not isinstance(X, torch.Tensor) or not isinstance(W, torch.Tensor) or not isinstance(tgt, torch.Tensor):
+        raise TypeError("X, W and tgt must be torch tensors")
+    dt = X.dtype
+    if dt is not torch.bfloat16 and dt is not torch.float32:
         raise ValueError("X must be bf16 or fp32")
     if X.dim() != 2 or W.dim() != 2:
         raise ValueError(f"expected X [rows, hidden] and W [vocab, hidden], got {tuple(X.shape)} and {tuple(W.shape)}")
-    _need(X, X.shape, X.dtype, "X")
-    _need(W, (W.shape[0], X.shape[1]), X.dtype, "W")
-    _need(tgt_ptr, (X.shape[0] + 1,), torch.int32, "tgt_ptr")
-    _need(tgt, (tgt.numel(),), torch.int32, "tgt")
-    _same_device(X, (W, "W"), (tgt_ptr, "tgt_ptr"), (tgt, "tgt"))
-    return LogprobDesc(X.shape[0], tgt.numel(), X.shape[1], W.shape[0], float(logit_scale),
-                       PSATTN_BF16 if X.dtype == torch.bfloat16 else PSATTN_FP32)
+    (n, h), v, e, index = X.shape, W.shape[0], tgt.numel(), X.get_device()
+    if index < 0 or not X.is_contiguous():
+        _need(X, X.shape, dt, "X")
+    _expect(W, (v, h), dt, index, "W")
+    _expect(tgt_ptr, (n + 1,), torch.int32, index, "tgt_ptr")
+    _expect(tgt, (e,), torch.int32, index, "tgt")
+    return LogprobDesc(n, e, h, v, logit_scale, PSATTN_BF16 if dt is torch.bfloat16 else PSATTN_FP32), n, e, h, v, index
 
 
-def _logprob_ws(desc, pass_, ws, X):
-    import torch
+@functools.lru_cache(maxsize=256)
+def _logprob_ws_bytes(rows, targets, hidden, vocab, dtype, pass_):
     n = ctypes.c_size_t()
-    _check(lib().psattn_logprob_workspace_size(ctypes.byref(desc), pass_, ctypes.byref(n)))
+    _check(lib().psattn_logprob_workspace_size(ctypes.byref(LogprobDesc(rows, targets, hidden, vocab, 1.0, dtype)), pass_, ctypes.byref(n)))
+    return n.value
+
+
+def _logprob_ws(desc, pass_, ws, X, index):
+    import torch
     if ws is None:
-        ws = torch.empty(n.value, dtype=torch.uint8, device=X.device)
-    _need(ws, (ws.numel(),), torch.uint8, "ws")
-    _same_device(X, (ws, "ws"))
+        return torch.empty(_logprob_ws_bytes(desc.rows, desc.targets, desc.hidden, desc.vocab, desc.dtype, pass_), dtype=torch.uint8, device=X.device)
+    _expect(ws, (ws.numel(),), torch.uint8, index, "ws")
     return ws
 
 
 def psattn_logprob_workspace_size(rows: int, targets: int, hidden: int, vocab: int, dtype: str = "bf16", pass_: int = 0) -> int:
     """Workspace bytes of psattn_logprob_fwd (pass 0) or psattn_logprob_bwd (1)."""
-    n = ctypes.c_size_t()
-    desc = LogprobDesc(int(rows), int(targets), int(hidden), int(vocab), 1.0, PSATTN_BF16 if dtype == "bf16" else PSATTN_FP32)
-    _check(lib().psattn_logprob_workspace_size(ctypes.byref(desc), int(pass_), ctypes.byref(n)))
-    return n.value
+    return _logprob_ws_bytes(int(rows), int(targets), int(hidden), int(vocab), PSATTN_BF16 if dtype == "bf16" else PSATTN_FP32, int(pass_))
 
 
 def psattn_logprob_fwd(X, W, tgt_ptr, tgt, logit_scale: float = 1.0, logp=None, LSE=None, ws=None):
@@ -654,18 +675,19 @@ def psattn_logprob_fwd(X, W, tgt_ptr, tgt, logit_scale: float = 1.0, logp=None, 
     returns (logp [targets], LSE [rows]), fp32.  X [rows, hidden] and W [vocab, hidden] (bf16 or fp32); row r's targets are
     tgt[tgt_ptr[r]:tgt_ptr[r + 1]] (int32; one outside the vocabulary has logp 0)."""
     import torch
-    desc = _logprob_args(X, W, tgt_ptr, tgt, logit_scale)
+    desc, n, e, h, v, index = _logprob_args(X, W, tgt_ptr, tgt, logit_scale)
+    f32 = torch.float32
     if logp is None:
-        logp = torch.empty(tgt.numel(), dtype=torch.float32, device=X.device)
+        logp = torch.empty(e, dtype=f32, device=X.device)
+    else:
+        _expect(logp, (e,), f32, index, "logp")
     if LSE is None:
-        LSE = torch.empty(X.shape[0], dtype=torch.float32, device=X.device)
-    _need(logp, (tgt.numel(),), torch.float32, "logp")
-    _need(LSE, (X.shape[0],), torch.float32, "LSE")
-    _same_device(X, (logp, "logp"), (LSE, "LSE"))
-    ws = _logprob_ws(desc, 0, ws, X)
-    with torch.cuda.device(X.device):
-        _check(lib().psattn_logprob_fwd(ctypes.byref(desc), _vp(X), _vp(W), _vp(tgt_ptr), _vp(tgt), _vp(logp), _vp(LSE), _vp(ws),
-                                        ws.numel(), ctypes.c_void_p(torch.cuda.current_stream(X.device).cuda_stream)))
+        LSE = torch.empty(n, dtype=f32, device=X.device)
+    else:
+        _expect(LSE, (n,), f32, index, "LSE")
+    ws = _logprob_ws(desc, 0, ws, X, index)
+    _on(index, lib().psattn_logprob_fwd, ctypes.byref(desc), X.data_ptr(), W.data_ptr(), tgt_ptr.data_ptr(), tgt.data_ptr(),
+        logp.data_ptr(), LSE.data_ptr(), ws.data_ptr(), ws.numel())
     return logp, LSE
 
 
@@ -674,23 +696,21 @@ def psattn_logprob_bwd(X, W, tgt_ptr, tgt, LSE, dlogp, logit_scale: float = 1.0,
     """Gradients (dX, dW) of the log-probabilities for their adjoints dlogp [targets] (fp32), in the inputs' dtype; None
     for one that is not needed.  LSE is the forward's.  Rows without a target of non-zero dlogp give 0, whatever they hold."""
     import torch
-    desc = _logprob_args(X, W, tgt_ptr, tgt, logit_scale)
-    _need(LSE, (X.shape[0],), torch.float32, "LSE")
-    _need(dlogp, (tgt.numel(),), torch.float32, "dlogp")
-    need_dX, need_dW = need_dX or dX is not None, need_dW or dW is not None
-    if need_dX and dX is None:
+    desc, n, e, h, v, index = _logprob_args(X, W, tgt_ptr, tgt, logit_scale)
+    _expect(LSE, (n,), torch.float32, index, "LSE")
+    _expect(dlogp, (e,), torch.float32, index, "dlogp")
+    if dX is not None:
+        _expect(dX, (n, h), X.dtype, index, "dX")
+    elif need_dX:
         dX = torch.empty_like(X)
-    if need_dW and dW is None:
+    if dW is not None:
+        _expect(dW, (v, h), X.dtype, index, "dW")
+    elif need_dW:
         dW = torch.empty_like(W)
-    for x, like, name in ((dX, X, "dX"), (dW, W, "dW")):
-        if x is not None:
-            _need(x, like.shape, X.dtype, name)
-    _same_device(X, (LSE, "LSE"), (dlogp, "dlogp"), (dX, "dX"), (dW, "dW"))
-    ws = _logprob_ws(desc, 1, ws, X)
-    with torch.cuda.device(X.device):
-        _check(lib().psattn_logprob_bwd(ctypes.byref(desc), _vp(X), _vp(W), _vp(tgt_ptr), _vp(tgt), _vp(LSE), _vp(dlogp), _vp(dX),
-                                        _vp(dW), _vp(ws), ws.numel(),
-                                        ctypes.c_void_p(torch.cuda.current_stream(X.device).cuda_stream)))
+    ws = _logprob_ws(desc, 1, ws, X, index)
+    _on(index, lib().psattn_logprob_bwd, ctypes.byref(desc), X.data_ptr(), W.data_ptr(), tgt_ptr.data_ptr(), tgt.data_ptr(),
+        LSE.data_ptr(), dlogp.data_ptr(), None if dX is None else dX.data_ptr(), None if dW is None else dW.data_ptr(), ws.data_ptr(),
+        ws.numel())
     return dX, dW
 
 
@@ -774,13 +794,11 @@ class AdamW:
         size = ctypes.c_size_t()
         _check(L.psattn_adamw_device_bytes(h, ctypes.byref(size)))
         self._table = torch.empty(size.value, dtype=torch.uint8, device=self.device)
-        with torch.cuda.device(self.device):
-            _check(L.psattn_adamw_upload(h, _vp(self._table), size.value,
-                                         ctypes.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)))
+        self._index = self.params[0].get_device()
+        _on(self._index, L.psattn_adamw_upload, h, self._table.data_ptr(), size.value)
         _check(L.psattn_adamw_workspace_size(h, ctypes.byref(size)))
         self._ws_bytes = size.value
         self._sizes = [p.numel() for p in self.params]
-        self._index = self.params[0].get_device()
 
     def __del__(self):
         if getattr(self, "_handle", None) is not None and _LIB is not None:
@@ -794,21 +812,23 @@ class AdamW:
         where that is not finite); the norm before clipping is then returned (fp32 [1]), else None.  ``dyn`` (int32 [4] on
         the GPU, see :meth:`dyn`): lr, grad_scale, step and seed are read from it instead, also by replays of a captured step."""
         import torch
-        T, f32, device = torch.Tensor, torch.float32, self.device
+        T, f32, bf16, device = torch.Tensor, torch.float32, torch.bfloat16, self.device
         n = len(self.params)
         if len(grads) != n:
             raise ValueError(f"{len(grads)} gradients for {n} weights")
-        given = [g for g in grads if g is not None]
-        kinds = set(map(_dtype_of, given))
-        # (whole lists at a time: a step over hundreds of small tensors is bound by these checks)
-        if not (list(map(T.numel, given)) == [k for k, g in zip(self._sizes, grads) if g is not None] and all(map(T.is_contiguous, given))
-                and kinds <= {f32, torch.bfloat16} and set(map(T.get_device, given)) <= {self._index}):
-            for i, (g, k) in enumerate(zip(grads, self._sizes)):
-                if g is not None and (g.numel() != k or g.dtype not in (f32, torch.bfloat16) or g.device != device or not g.is_contiguous()):
-                    raise ValueError(f"grads[{i}]: expected {k} contiguous bf16 or fp32 elements on {device}, got {g.dtype} {tuple(g.shape)} on {g.device}")
-        if len(given) == n:
+        # Whole lists at a time: a step over hundreds of small tensors is bound by these checks.
+        try:
+            kinds = set(map(_dtype_of, grads))
+            fits = (list(map(T.numel, grads)) == self._sizes and kinds <= {f32, bf16} and all(map(T.is_contiguous, grads))
+                    and set(map(T.get_device, grads)) == {self._index})
+        except (AttributeError, TypeError):     # a None among them
+            kinds, fits = set(), False
+        if fits:
             pointers = np.fromiter(map(T.data_ptr, grads), np.uint64, n)
         else:
+            for i, (g, k) in enumerate(zip(grads, self._sizes)):
+                if g is not None and (g.numel() != k or g.dtype not in (f32, bf16) or g.device != device or not g.is_contiguous()):
+                    raise ValueError(f"grads[{i}]: expected {k} contiguous bf16 or fp32 elements on {device}, got {g.dtype} {tuple(g.shape)} on {g.device}")
             pointers = np.array([0 if g is None else g.data_ptr() for g in grads], np.uint64)
         if len(kinds) == 1:
             dtypes = np.full(n, PSATTN_FP32 if f32 in kinds else PSATTN_BF16, np.int32)
@@ -820,9 +840,8 @@ class AdamW:
         norm = torch.empty(1, dtype=f32, device=device) if max_norm > 0 else None
         ws = torch.empty(self._ws_bytes, dtype=torch.uint8, device=device)
         hyper = AdamwHyper(lr, betas[0], betas[1], eps, weight_decay, max_norm, grad_scale, step, seed & 0xffffffff, 0)
-        with torch.cuda.device(device):
-            _check(lib().psattn_adamw_step(self._handle, _ptr(pointers, ctypes.c_void_p), _ptr(dtypes, ctypes.c_int32), ctypes.byref(hyper), _vp(dyn), _vp(norm), _vp(ws), self._ws_bytes,
-                                           ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)))
+        _on(self._index, lib().psattn_adamw_step, self._handle, pointers.ctypes.data, dtypes.ctypes.data, ctypes.byref(hyper),
+            None if dyn is None else dyn.data_ptr(), None if norm is None else norm.data_ptr(), ws.data_ptr(), self._ws_bytes)
         return norm
 
     def dyn(self, lr: float, step: int, grad_scale: float = 1.0, seed: int = 0, out=None):

@@ -1351,10 +1351,11 @@ struct LogprobPlan {
 struct LogprobTiling { int32_t shape, splits, stages; double us; };
 LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes, int max_splits) {
   struct Kind { int32_t shape, m, n, slots; double stage, ends; };
-  static const Kind kinds[] = {{LP_LARGE, 256, 256, 256, 1.5, 10}, {LP_SMALL, 128, 128, 512, 0.83, 8}, {LP_DEEP, 128, 128, 256, 0.5, 8}};
+  static const std::vector<Kind> bf16 = {{LP_LARGE, 256, 256, 256, 1.5, 10}, {LP_SMALL, 128, 128, 512, 0.83, 8}, {LP_DEEP, 128, 128, 256, 0.5, 8}};
+  static const std::vector<Kind> fp32 = {{LP_LARGE, 256, 128, 256, 4.1, 12}, {LP_SMALL, 128, 128, 256, 3.2, 10}};
   LogprobTiling best{LP_LARGE, 1, 1, 1e30};
   const int64_t nk = std::max<int64_t>(1, (k + 63) / 64);
-  for (const Kind& c : kinds) {
+  for (const Kind& c : planes == 3 ? fp32 : bf16) {
     const int64_t tiles = ((down + c.m - 1) / c.m) * ((across + c.n - 1) / c.n);
     for (int64_t s = 1; s <= max_splits && s <= nk; ++s) {
       const int64_t each = (nk + s - 1) / s, parts = (nk + each - 1) / each;
@@ -1362,7 +1363,7 @@ LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes
       const double r = (double)(tiles * s) / c.slots, rounds = std::ceil(r);
       const double slabs = (double)s * (double)down * (double)across * 4;
       if (s > 1 && slabs > (double)((int64_t)512 << 20)) break;
-      const double us = (rounds + std::max(r, 1.0)) / 2 * ((double)each * (planes == 3 ? 6 : 1) * c.stage + c.ends) +
+      const double us = (rounds + std::max(r, 1.0)) / 2 * ((double)each * c.stage + c.ends) +
                         (s > 1 ? 6 + slabs * 2 / 4.5e6 : 0);
       if (us < best.us) best = {c.shape, (int32_t)s, (int32_t)each, us};
     }

@@ -16,17 +16,32 @@ namespace {
 
 using namespace dev;
 
-// The workgroups' shapes: WM x WN wavefronts, each with FM x FN tiles of 32 x 32; stages of BK elements of the summed dimension,
-// RING of them in LDS.
-template <int WM_, int WN_, int FM_, int FN_, int BK_, int RING_>
-struct Shape2 {
+// The workgroups' shapes: WM x WN wavefronts, each with FM x FN tiles of 32 x 32; stages of BK elements of the summed dimension
+// of each of P planes, RING of them in LDS.
+template <int WM_, int WN_, int FM_, int FN_, int BK_, int RING_, int P_>
+struct Tiling {
   static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, WAVES = WM * WN, THREADS = 64 * WAVES, M = 32 * WM * FM, N = 32 * WN * FN;
-  static constexpr int BK = BK_, RING = RING_, STAGE = (M + N) * BK * 2, LDS = RING * STAGE;
+  static constexpr int BK = BK_, RING = RING_, P = P_, PLANE = (M + N) * BK * 2, STAGE = P * PLANE, LDS = RING * STAGE;
 };
-using Large = Shape2<2, 4, 4, 2, 64, 2>;    // 256 x 256, one workgroup per CU
-using Small = Shape2<2, 2, 2, 2, 64, 2>;    // 128 x 128, two
-using Deep = Shape2<2, 2, 2, 2, 64, 4>;     // 128 x 128, one, three stages ahead
-using Thin = Shape2<4, 1, 1, 1, 64, 6>;     // 128 x 32, one: 100 KB of copies on their way
+template <int P>
+struct Tilings;
+template <>
+struct Tilings<1> {
+  using Large = Tiling<2, 4, 4, 2, 64, 2, 1>;    // 256 x 256, one workgroup per CU
+  using Small = Tiling<2, 2, 2, 2, 64, 2, 1>;    // 128 x 128, two
+  using Deep = Tiling<2, 2, 2, 2, 64, 4, 1>;     // 128 x 128, one, three stages ahead
+  using Thin = Tiling<4, 1, 1, 1, 64, 6, 1>;     // 128 x 32, one: 100 KB of copies on their way
+};
+// All planes of a stage lie in LDS together, so that each is copied, and read into registers, once for its products with three,
+// two or one of the other operand's: half the copies and reads of a pass per pair of planes (513 rows x 1024 x 16001: logits
+// 150 us that way).  One workgroup per CU.
+template <>
+struct Tilings<3> {
+  using Large = Tiling<4, 2, 2, 2, 32, 2, 3>;    // 256 x 128
+  using Small = Tiling<2, 2, 2, 2, 32, 2, 3>;    // 128 x 128
+  using Deep = Small;
+  using Thin = Tiling<4, 1, 1, 1, 64, 2, 3>;     // 128 x 32
+};
 
 // An operand of a product: element (i, k) of plane q at p + q plane + i ld + k, or + k ld + i where K is the outer dimension.
 // Reads of i >= rows and k >= ks give some element of the operand in their place: such i are not stored, and at
@@ -119,7 +134,7 @@ struct Reader {
 // a multiple of 64).  RING stages in LDS: while one is multiplied, the next RING - 1 are on their way.  The barrier
 // between two stages stands before the last of a stage's products, whose operands are in registers by then, so
 // that they cover the first reads of the next stage.
-template <class S, int PLANES, bool KA, bool KB>
+template <class S, bool KA, bool KB>
 __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Operand& A, const Operand& B, int64_t i0, int64_t j0, int ks,
                                         uint8_t* lds) {
   constexpr int BK = S::BK, QS = BK / 16;
@@ -130,7 +145,8 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
     for (int g = 0; g < S::FN; ++g)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[f][g][e] = 0.f;
-  const int nk = max(0, ks + 63) / 64 * (64 / BK), steps = PLANES == 3 ? 6 * nk : nk;
+  constexpr int P = S::P;
+  const int steps = max(0, ks + 63) / 64 * (64 / BK);
   if (steps == 0) return;
   using LA = Loader<S::M, BK, S::WAVES, KA>;
   using LB = Loader<S::N, BK, S::WAVES, KB>;
@@ -139,44 +155,36 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
   const Reader<S::M, BK, S::FM, KA> ra(wave / S::WN * S::FM * 32, lane);
   const Reader<S::N, BK, S::FN, KB> rb(wave % S::WN * S::FN * 32, lane);
   const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(lds));
-  const int inside = min(A.ks, B.ks), whole = inside / BK;   // stages that lie wholly inside both operands
+  const int whole = min(A.ks, B.ks) / BK;   // stages that lie wholly inside both operands
   la.aim(A, i0, BK, wave, lane);
   lb.aim(B, j0, BK, wave, lane);
-  int pair = 0, kt = 0, fill = 0;
-  const char* pa = (const char*)(la.p + (PLANES == 3 ? 2 * A.plane : 0));
-  const char* pb = (const char*)lb.p;
-  const char *qa, *qb;       // the stage that is being copied, and where to
+  int kt = 0, fill = 0;
+  const char *qa[P], *qb[P];   // the planes of the stage that is being copied, and where to
   uint32_t da, db;
   auto point = [&] {
-    qa = pa, qb = pb;
-    if (whole < nk && (kt >= whole || kt == 0)) {   // (the last stages of a plane, and the first behind them)
+    int ta = kt, tb = kt;
+    if (kt >= whole) {   // (the last stages)
       int ka = A.ks - kt * BK, kb = B.ks - kt * BK;
-      if (ka <= 0) qa = pa - kt * la.step, ka = A.ks;   // wholly behind the operand's end: its first stage again
-      if (kb <= 0) qb = pb - kt * lb.step, kb = B.ks;
+      if (ka <= 0) ta = 0, ka = A.ks;   // wholly behind the operand's end: its first stage again
+      if (kb <= 0) tb = 0, kb = B.ks;
       la.aim(A, i0, min(BK, ka), wave, lane);
       lb.aim(B, j0, min(BK, kb), wave, lane);
     }
-    qa = uniform(qa);
-    qb = uniform(qb);
+#pragma unroll
+    for (int q = 0; q < P; ++q) {
+      qa[q] = uniform((const char*)(la.p + q * A.plane) + ta * la.step);
+      qb[q] = uniform((const char*)(lb.p + q * B.plane) + tb * lb.step);
+    }
     da = at + fill * S::STAGE + wave * LA::COUNT * 1024;
     db = at + fill * S::STAGE + S::M * BK * 2 + wave * LB::COUNT * 1024;
     if (++fill == S::RING) fill = 0;
     ++kt;
-    pa += la.step;
-    pb += lb.step;
-    if (PLANES == 3 && kt == nk) {
-      kt = 0;
-      ++pair;   // the planes of A and B: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
-      const int ia = pair == 1 || pair == 3 ? 1 : 0, ib = pair == 2 ? 2 : pair == 1 || pair == 4 ? 1 : 0;
-      pa = (const char*)(la.p + ia * A.plane);
-      pb = (const char*)(lb.p + ib * B.plane);
-    }
   };
-  constexpr int COPIES = LA::COUNT + LB::COUNT;
+  constexpr int COPIES = P * (LA::COUNT + LB::COUNT);
   auto copy = [&](auto j) {
-    constexpr int J = decltype(j)::value;
-    if constexpr (J < LA::COUNT) la.template issue<J>(qa, da);
-    else lb.template issue<J - LA::COUNT>(qb, db);
+    constexpr int Q = decltype(j)::value / (LA::COUNT + LB::COUNT), J = decltype(j)::value % (LA::COUNT + LB::COUNT);
+    if constexpr (J < LA::COUNT) la.template issue<J>(qa[Q], da + Q * S::PLANE);
+    else lb.template issue<J - LA::COUNT>(qb[Q], db + Q * S::PLANE);
   };
   auto issue = [&] {
     point();
@@ -188,23 +196,24 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
     else wait_vmem<0>();
     barrier_only();
   };
-  bf16x8 fa[2][S::FM], fb[2][S::FN];
+  bf16x8 fa[2][P][S::FM], fb[2][P][S::FN];
   for (int s = 0; s < S::RING - 1 && s < steps; ++s) issue();
   landed(S::RING - 1 <= steps);
   if (S::RING - 1 < steps) issue();
-  // fragment F of the operands' FM + FN, elements 16 KK .. of a stage
+  // fragment F of the operands' P (FM + FN), elements 16 KK .. of a stage
+  constexpr int READS = P * (S::FM + S::FN);
   auto read = [&](auto kk, auto frag, const uint8_t* tile) {
-    constexpr int KK = decltype(kk)::value, F = decltype(frag)::value;
-    if constexpr (F < S::FM) fa[KK & 1][F] = ra.template read<KK, F>(tile);
-    else fb[KK & 1][F - S::FM] = rb.template read<KK, F - S::FM>(tile + S::M * BK * 2);
+    constexpr int KK = decltype(kk)::value, Q = decltype(frag)::value / (S::FM + S::FN), F = decltype(frag)::value % (S::FM + S::FN);
+    if constexpr (F < S::FM) fa[KK & 1][Q][F] = ra.template read<KK, F>(tile + Q * S::PLANE);
+    else fb[KK & 1][Q][F - S::FM] = rb.template read<KK, F - S::FM>(tile + Q * S::PLANE + S::M * BK * 2);
   };
-  static_for<S::FM + S::FN>([&](auto f) { read(IntC<0>{}, f, lds); });
+  static_for<READS>([&](auto f) { read(IntC<0>{}, f, lds); });
   int use = 0;
   // One stage: COPY: a later stage is copied meanwhile, into this one's place; NEXT: a stage follows.  Between two products of
   // a wavefront stands one read of the operands of the products behind this quarter, or a copy.
   auto stage = [&](auto copy_flag, auto next_flag) {
     constexpr bool COPY = decltype(copy_flag)::value, NEXT = decltype(next_flag)::value;
-    constexpr int PRODUCTS = S::FM * S::FN, READS = S::FM + S::FN;
+    constexpr int PRODUCTS = (P == 3 ? 6 : 1) * S::FM * S::FN;
     const uint8_t* tile = lds + use * S::STAGE;
     if (++use == S::RING) use = 0;
     const uint8_t* next = lds + use * S::STAGE;
@@ -220,8 +229,10 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
       }
       sched_fence();
       static_for<PRODUCTS>([&](auto m) {
-        constexpr int I = decltype(m)::value, F = I / S::FN, G = I % S::FN;
-        acc[F][G] = mfma(fa[KK & 1][F], fb[KK & 1][G], acc[F][G]);
+        constexpr int I = decltype(m)::value, F = I / S::FN % S::FM, G = I % S::FN, PAIR = I / (S::FM * S::FN);
+        // the planes of A and B: (2, 0) (1, 1) (0, 2) (1, 0) (0, 1) (0, 0)
+        constexpr int QA = P == 1 ? 0 : PAIR == 0 ? 2 : PAIR == 1 || PAIR == 3 ? 1 : 0, QB = P == 1 ? 0 : PAIR == 2 ? 2 : PAIR == 1 || PAIR == 4 ? 1 : 0;
+        acc[F][G] = mfma(fa[KK & 1][QA][F], fb[KK & 1][QB][G], acc[F][G]);
         sched_fence();
         static_for<PER>([&](auto j) {
           constexpr int A = I * PER + decltype(j)::value;
@@ -280,8 +291,8 @@ __device__ __forceinline__ void store_tile(F&& eight, bf16_t* out, int64_t ld, i
 
 // Which part of the sum and which tile a workgroup takes.  Workgroups go to the 8 XCDs in turn; those of one XCD take
 // consecutive ones, part by part, and in a part in bands of 4 tiles down by all tiles across, so that the 32 that run on
-// it at a time share rows of both operands in its L2.  (dX of 513 fp32 rows x 1024 x 16001, 12 parts of 40 tiles: 171 us
-// with each part's tiles spread over the XCDs.)
+// it at a time share rows of both operands in its L2.  (dX of 513 fp32 rows x 1024 x 16001, 12 parts of 40 tiles: 172 us
+// with each part's tiles spread over the XCDs, 121 so.)
 struct Tile { int part, down, across; };
 __device__ __forceinline__ Tile tile_of(int downs, int acrosses) {
   const int each = gridDim.x / 8, rest = gridDim.x % 8, x = blockIdx.x % 8;
@@ -380,7 +391,7 @@ __global__ __launch_bounds__(256) void wplanes_kernel(LogprobArgs a, int piece) 
 }
 
 // ---- a tile of logits: M entries of the piece down, N rows across
-template <class S, int PLANES, bool BACKWARD>
+template <class S, bool BACKWARD>
 __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -393,7 +404,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
   if constexpr (BACKWARD)
     for (int j = threadIdx.x; j < S::N; j += S::THREADS)
       if (j0 + j < a.np) s_row[j] = a.row[j0 + j];
-  product<S, PLANES, false, false>(acc, W, x_operand(a), i0, j0, a.hp, lds);
+  product<S, false, false>(acc, W, x_operand(a), i0, j0, a.hp, lds);
   const float c = a.scale * kLog2e;
   const int left = W.rows - iw - 4 * (lane >> 5);   // element (f, e) is an entry where 32 f + down(e) is below
   if constexpr (!BACKWARD) {
@@ -465,7 +476,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[f][g][e] = 32 * f + down(e) < left ? acc[f][g][e] : 0.f;
       }
-      if (PLANES == 1) {
+      if (S::P == 1) {
         // A target's dz is most of its row's, so its rounding would be most of the gradients' error: what it leaves out
         // goes into them by itself.
         for (int t = row.e0; __any(t < row.e1); ++t) {
@@ -487,7 +498,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
     }
     bf16_t* out = a.dl + j0 * a.piece_v + i0;
     const int64_t lim_across = a.np - j0, lim_down = a.piece_v - i0;
-    if constexpr (PLANES == 1) {
+    if constexpr (S::P == 1) {
       store_tile<S>(
           [&](int f, int g, int h) {
             const f32x16& x = acc[f][g];
@@ -635,10 +646,10 @@ __device__ __forceinline__ float rem_of(const LogprobArgs& a, int e, int r) {
   return e >= e0 && e < e1 ? a.ent_rem[e] : 0.f;
 }
 // the workgroup's tile to a result of the inputs' type
-template <class S, int PLANES>
+template <class S>
 __device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::FM][S::FN], void* out, int64_t at, int64_t ld, int64_t lim_across, int64_t lim_down,
                                          uint8_t* lds) {
-  if constexpr (PLANES == 1) {
+  if constexpr (S::P == 1) {
     store_tile<S>(
         [&](int f, int g, int h) {
           const f32x16& x = acc[f][g];
@@ -659,7 +670,7 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::FM][S::FN], void
 }
 
 // dX: M of the hidden dimension down, N rows across
-template <class S, int PLANES>
+template <class S>
 __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -668,9 +679,9 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
   f32x16 acc[S::FM][S::FN];
-  const bool last = piece == a.pieces - 1, rest = PLANES == 1 && last && split == 0;   // rest: what the targets' dz left out is added
+  const bool last = piece == a.pieces - 1, rest = S::P == 1 && last && split == 0;   // rest: what the targets' dz left out is added
   // (the tile's rows have their targets one behind the other: LIST at a time, the first ones ahead of the products)
-  constexpr int LIST = PLANES == 1 ? 2 * S::N : 1;
+  constexpr int LIST = S::P == 1 ? 2 * S::N : 1;
   __shared__ struct { float rem; int32_t tgt, col; } s_list[LIST];
   int e_lo = 0, e_hi = 0;
   auto list = [&] {
@@ -686,7 +697,7 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
   }
   const Operand W = part_of(swapped(w_operand(a, piece)), true, (int64_t)split * k, k);
   const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.np, a.piece_v}, false, (int64_t)split * k, k);
-  product<S, PLANES, true, false>(acc, W, D, i0, j0, W.ks, lds);
+  product<S, true, false>(acc, W, D, i0, j0, W.ks, lds);
   float* sums = a.dx_acc + (int64_t)split * a.n * a.h;
 #pragma unroll
   for (int g = 0; g < S::FN; ++g) {
@@ -723,11 +734,11 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
       for (int f = 0; f < S::FM; ++f) put_rows(sums + r * a.h, iw + 32 * f, limit, acc[f][g], lane);
     }
   }
-  if (last && a.splits_dx == 1) put_tile<S, PLANES>(acc, a.dX, j0 * a.h + i0, a.h, a.n - j0, a.h - i0, lds);
+  if (last && a.splits_dx == 1) put_tile<S>(acc, a.dX, j0 * a.h + i0, a.h, a.n - j0, a.h - i0, lds);
 }
 
 // dW: M of the hidden dimension down, N entries across
-template <class S, int PLANES>
+template <class S>
 __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -739,10 +750,10 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
   const int v0 = piece * a.piece_v + (int)j0, vn = min(S::N, min(a.piece_v - (int)j0, a.v - v0));   // the tile's entries
   // What the targets' dz left out (rest): the targets are looked through for this tile's entries, 64 per wavefront and turn,
   // and those found are listed in their order, as many at a time as the list holds in any case.
-  constexpr int TURNS = 8, LIST = PLANES == 1 ? 256 * S::WAVES : 1;
+  constexpr int TURNS = 8, LIST = S::P == 1 ? 256 * S::WAVES : 1;
   __shared__ struct { float rem; int32_t row, col; } s_list[LIST];
   __shared__ int s_count[S::WAVES];
-  const bool rest = PLANES == 1 && split == 0;
+  const bool rest = S::P == 1 && split == 0;
   int listed = 0, seen = 0, taken = 0;   // of the batch from seen on, `taken` have been listed before
   auto collect = [&] {
     listed = 0;
@@ -794,7 +805,7 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
   if (rest) collect();
   const Operand X = part_of({a.xc, a.hp, (int64_t)a.np * a.hp, a.hp, a.np}, true, (int64_t)split * k, k);
   const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, a.np}, true, (int64_t)split * k, k);
-  product<S, PLANES, true, true>(acc, X, D, i0, j0, X.ks, lds);
+  product<S, true, true>(acc, X, D, i0, j0, X.ks, lds);
   if (rest) {
     for (;;) {
       add_terms<S>(
@@ -813,7 +824,7 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
       for (int f = 0; f < S::FM; ++f) put_rows(sums + (j0 + j) * a.h, iw + 32 * f, j < vn ? a.h : 0, acc[f][g], lane);
     }
   } else {
-    put_tile<S, PLANES>(acc, a.dW, (int64_t)v0 * a.h + i0, a.h, vn, a.h - i0, lds);
+    put_tile<S>(acc, a.dW, (int64_t)v0 * a.h + i0, a.h, vn, a.h - i0, lds);
   }
 }
 
@@ -850,26 +861,29 @@ void launch_tiles(K kernel, int64_t down, int64_t across, int parts, const Logpr
   const int d = tiles(down, S::M), c = tiles(across, S::N);
   hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)d * c * parts)), dim3(S::THREADS), 0, st, a, piece, d, c);
 }
-template <int PLANES, bool BACKWARD>
+template <int P, bool BACKWARD>
 void logits(const LogprobArgs& a, int piece, hipStream_t st) {
+  using T = Tilings<P>;
   const int rows = piece_rows(a, piece), n = BACKWARD ? a.np : a.n;
-  if (a.shape == LP_LARGE) launch_tiles<Large>(logits_kernel<Large, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
-  else if (a.shape == LP_SMALL) launch_tiles<Small>(logits_kernel<Small, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
-  else if (a.shape == LP_DEEP) launch_tiles<Deep>(logits_kernel<Deep, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
-  else launch_tiles<Thin>(logits_kernel<Thin, PLANES, BACKWARD>, rows, n, 1, a, piece, st);
+  if (a.shape == LP_LARGE) launch_tiles<typename T::Large>(logits_kernel<typename T::Large, BACKWARD>, rows, n, 1, a, piece, st);
+  else if (a.shape == LP_SMALL) launch_tiles<typename T::Small>(logits_kernel<typename T::Small, BACKWARD>, rows, n, 1, a, piece, st);
+  else if (a.shape == LP_DEEP) launch_tiles<typename T::Deep>(logits_kernel<typename T::Deep, BACKWARD>, rows, n, 1, a, piece, st);
+  else launch_tiles<typename T::Thin>(logits_kernel<typename T::Thin, BACKWARD>, rows, n, 1, a, piece, st);
 }
-template <int PLANES>
+template <int P>
 void dx(const LogprobArgs& a, int piece, hipStream_t st) {
-  if (a.shape_dx == LP_LARGE) launch_tiles<Large>(dx_kernel<Large, PLANES>, a.h, a.n, a.splits_dx, a, piece, st);
-  else if (a.shape_dx == LP_SMALL) launch_tiles<Small>(dx_kernel<Small, PLANES>, a.h, a.n, a.splits_dx, a, piece, st);
-  else launch_tiles<Deep>(dx_kernel<Deep, PLANES>, a.h, a.n, a.splits_dx, a, piece, st);
+  using T = Tilings<P>;
+  if (a.shape_dx == LP_LARGE) launch_tiles<typename T::Large>(dx_kernel<typename T::Large>, a.h, a.n, a.splits_dx, a, piece, st);
+  else if (a.shape_dx == LP_SMALL) launch_tiles<typename T::Small>(dx_kernel<typename T::Small>, a.h, a.n, a.splits_dx, a, piece, st);
+  else launch_tiles<typename T::Deep>(dx_kernel<typename T::Deep>, a.h, a.n, a.splits_dx, a, piece, st);
 }
-template <int PLANES>
+template <int P>
 void dw(const LogprobArgs& a, int piece, hipStream_t st) {
+  using T = Tilings<P>;
   const int rows = piece_rows(a, piece);
-  if (a.shape_dw == LP_LARGE) launch_tiles<Large>(dw_kernel<Large, PLANES>, a.h, rows, a.splits_dw, a, piece, st);
-  else if (a.shape_dw == LP_SMALL) launch_tiles<Small>(dw_kernel<Small, PLANES>, a.h, rows, a.splits_dw, a, piece, st);
-  else launch_tiles<Deep>(dw_kernel<Deep, PLANES>, a.h, rows, a.splits_dw, a, piece, st);
+  if (a.shape_dw == LP_LARGE) launch_tiles<typename T::Large>(dw_kernel<typename T::Large>, a.h, rows, a.splits_dw, a, piece, st);
+  else if (a.shape_dw == LP_SMALL) launch_tiles<typename T::Small>(dw_kernel<typename T::Small>, a.h, rows, a.splits_dw, a, piece, st);
+  else launch_tiles<typename T::Deep>(dw_kernel<typename T::Deep>, a.h, rows, a.splits_dw, a, piece, st);
 }
 void sum_slabs(const LogprobArgs& a, const float* slab, int64_t stride, int count, void* out, int64_t n, hipStream_t st) {
   const dim3 grid((unsigned)std::min<int64_t>((n / 4 + 255) / 256, 8192));

@@ -69,6 +69,20 @@ def test_fp32_states(wdt, gdt):
                 assert torch.equal(params[i], opt.master[i].bfloat16())
 
 
+def test_each_operation_is_rounded_by_itself():
+    """Bit for bit the step that fp32 tensor operations give one after the other (torch's are IEEE)."""
+    from paper_2608_25683_amd import psattn as P
+    n = 5003
+    w, m, v, g = draw((n,), 1), draw((n,), 2, sigma=0.1), draw((n,), 3).square(), draw((n,), 4)
+    p = [w.clone()]
+    opt = P.AdamW(p, state={"m": [m.clone()], "v": [v.clone()]})
+    opt.step([g], step=4, **HYPER)
+    (b1, b2), lr = HYPER["betas"], HYPER["lr"]
+    mm, vv = m * b1 + g * (1 - b1), v * b2 + (g * g) * (1 - b2)
+    ww = w * (1 - lr * 0.1) - (mm / (vv.sqrt() * (1 / (1 - b2 ** 4) ** 0.5) + 1e-8)) * (lr / (1 - b1 ** 4))
+    assert torch.equal(opt.m[0], mm) and torch.equal(opt.v[0], vv) and torch.equal(p[0], ww)
+
+
 @pytest.mark.parametrize("wdt", ["bf16", "fp32"])
 def test_8_bit_states(wdt):
     from paper_2608_25683_amd import psattn as P

@@ -94,8 +94,12 @@ def check(got, ref, err, what):
         assert not bad.any(), f"{k}: {int(bad.sum())} of {bad.numel()} elements, worst {worst:.3g} of the bound"
 
 
+# from one element to several tiles of every size the kernels use (32, 128 and 256 rows, 128 and 256 entries), odd ones among
+# them, with the summed dimension short of a stage, a stage and one more element, and split over workgroups (dX: vocabularies
+# above 512 behind few rows; dW: many rows before few entries)
 SHAPES = [(1, 8, 1), (1, 64, 7), (2, 72, 300), (63, 128, 129), (64, 8, 128), (65, 136, 257), (130, 264, 1001), (257, 64, 2500),
-          (300, 192, 515), (9, 520, 4100), (520, 256, 770)]
+          (300, 192, 515), (9, 520, 4100), (520, 256, 770),
+          (32, 64, 640), (33, 1032, 385), (1500, 16, 140), (5, 2056, 96)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
@@ -166,6 +170,40 @@ def test_one_gradient_alone_is_the_same(dtype):
     assert b is None and torch.equal(a, dx)
     a, b = P.psattn_logprob_bwd(x, w, ptr, tgt, lse, g, need_dX=False)
     assert a is None and torch.equal(b, dw)
+
+
+def test_one_token_is_the_target_of_all_rows():
+    """More targets in one tile than its list holds at a time (4096 of them), and rows with hundreds of targets."""
+    n, h, v = 4500, 64, 300
+    x, w, ptr, tgt, g = make(n, h, v, "bf16", 61, per_row=[1] * n)
+    tgt[:] = 77
+    tgt[::1000] = 299
+    got = call(x, w, ptr, tgt, g)
+    xd, wd, gd = x.double(), w.double(), g.double()
+    z = xd @ wd.t()
+    p = torch.softmax(z, 1)
+    dz = -gd[:, None] * p
+    dz[torch.arange(n), tgt.long()] += gd
+    # dz and the results are rounded once each (uniform in a binade: 2^-8.8 in the mean square at most)
+    for name, ref in (("dX", dz @ wd), ("dW", dz.t() @ xd)):
+        rel = float((got[name].double().cpu() - ref).norm() / ref.norm())
+        assert rel <= 2 * 2.0 ** -8.8, (name, rel)
+    a = make(7, h, v, "bf16", 62, per_row=[0, 700, 1, 0, 333, 2, 900])
+    check(call(*a), *reference(*a, 1.0), "hundreds of targets")
+
+
+def test_rounding_of_a_targets_dz_does_not_reach_the_gradients():
+    """The dz of a row's target is most of it; its rounding to bf16 alone would be 2^-9.8 of dX in the mean square beside the
+    result's own, sqrt(2) of that together.  What it leaves out is added, so the whole error stays within 1.15 of the result's
+    own rounding, measured on the exact result."""
+    x, w, ptr, tgt, g = make(512, 256, 3000, "bf16", 71, per_row=[1] * 512)
+    got = call(x, w, ptr, tgt, g)
+    xd, wd, gd = x.cuda().double(), w.cuda().double(), g.cuda().double()
+    dz = -gd[:, None] * torch.softmax(xd @ wd.t(), 1)
+    dz[torch.arange(512, device="cuda"), tgt.cuda().long()] += gd
+    for name, ref in (("dX", dz @ wd), ("dW", dz.t() @ xd)):
+        own = float((ref.bfloat16().double() - ref).norm())
+        assert float((got[name].double() - ref).norm()) <= 1.15 * own, name
 
 
 def test_confident_rows():

@@ -88,15 +88,24 @@ __device__ __forceinline__ f32x4 decode(uint32_t codes, int e) {
                __builtin_amdgcn_cvt_f32_fp8(codes, 2) * p, __builtin_amdgcn_cvt_f32_fp8(codes, 3) * p};
 }
 
-// max of x over the wavefront's 64 lanes
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int w = 32; w >= 1; w >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, w));
-  return x;
+// biased exponent of x, 0 if x is not finite
+__device__ __forceinline__ uint32_t exponent(float x) {
+  const uint32_t e = __float_as_uint(x) >> 23 & 0xffu;
+  return e == 0xffu ? 0u : e;
 }
-__device__ __forceinline__ uint32_t magnitude(float x) {   // bits of |x|, 0 if x is not finite
-  const uint32_t u = __float_as_uint(x) & 0x7fffffffu;
-  return u < 0x7f800000u ? u : 0u;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+__device__ __forceinline__ u16x2 max2(u16x2 a, u16x2 b) { return __builtin_elementwise_max(a, b); }
+template <int ROTATE>
+__device__ __forceinline__ u16x2 max_rotated(u16x2 x) {   // with the lane ROTATE further among 16
+  const int y = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + ROTATE, 0xf, 0xf, true);
+  return max2(x, __builtin_bit_cast(u16x2, y));
+}
+// both halves' max over the wavefront's 64 lanes, the same in every lane
+__device__ __forceinline__ u16x2 wave_max(u16x2 x) {
+  x = max_rotated<1>(max_rotated<2>(max_rotated<4>(max_rotated<8>(x))));
+  const int y = __builtin_bit_cast(int, x);
+  auto row = [&](int lane) { return __builtin_bit_cast(u16x2, __builtin_amdgcn_readlane(y, lane)); };
+  return max2(max2(row(0), row(16)), max2(row(32), row(48)));
 }
 
 // x to its e4m3 value on the block's grid (as a float), up or down by the 16 random bits; above 2^-6 of the grid its codes
@@ -152,16 +161,17 @@ __device__ __forceinline__ void step_chunk(const AdamwTensor& t, P* weights, con
     store4(weights, i, n, w);
     if (t.bf16) store4((bf16_t*)t.param, i, n, w);
     if (BITS == 8) {
-      uint32_t tm = 0, tr = 0;
       f32x4 ym, yr;
+      u16x2 top = {0, 0};   // (elements behind the tensor's end have m = v = 0)
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < n) tm = max(tm, magnitude(m[k])), tr = max(tr, magnitude(r[k]));
-      const int em = max((int)(wave_max(tm) >> 23) - 7, 1), er = max((int)(wave_max(tr) >> 23) - 7, 1);
+      for (int k = 0; k < 4; ++k) top = max2(top, u16x2{(uint16_t)exponent(m[k]), (uint16_t)exponent(r[k])});
+      top = wave_max(top);
+      const int em = max((int)top[0] - 7, 1), er = max((int)top[1] - 7, 1);
       const float im = __uint_as_float((uint32_t)(254 - em) << 23), ir = __uint_as_float((uint32_t)(254 - er) << 23);
+      const uint32_t h0 = (uint32_t)i * 0x9E3779B1u;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint32_t h = adamw_mix(((uint32_t)(i + k) * 0x9E3779B1u) ^ key);
+        const uint32_t h = adamw_mix((h0 + k * 0x9E3779B1u) ^ key);
         ym[k] = to_code<false>(m[k], im, h >> 16);
         yr[k] = to_code<true>(r[k], ir, h & 0xffffu);
       }
@@ -231,7 +241,7 @@ __global__ __launch_bounds__(1024) void adamw_scalars_kernel(AdamwArgs a, int wi
   PSATTN_NO_CONTRACT
   double x = 0;
   if (with_norm)
-#pragma unroll 8
+#pragma unroll 16
     for (int i = threadIdx.x; i < a.total_items; i += 1024) x += a.part[i];
   x = block_sum<1024>(x);
   if (threadIdx.x) return;

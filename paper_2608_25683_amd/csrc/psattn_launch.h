@@ -104,7 +104,7 @@ struct AdamwTensor {
   int32_t bf16;
 };
 struct AdamwItem { int32_t tensor, chunk; };      // elements chunk * ADAMW_CHUNK ... of a tensor
-constexpr int ADAMW_CHUNK = 8192, ADAMW_BLOCK = 256;
+constexpr int ADAMW_CHUNK = 4096, ADAMW_BLOCK = 256;
 constexpr int ADAMW_GRADS = 320;                  // gradient pointers of a launch, in its 4 KB of arguments
 struct AdamwGrads {
   const void* g[ADAMW_GRADS];

@@ -731,62 +731,61 @@ class AdamW:
         self._handle = None
         self.params = list(params)
         self.state_bits = int(state_bits)
-        if not self.params:
+        n, f32, bf16, u8, e4m3 = len(self.params), torch.float32, torch.bfloat16, torch.uint8, torch.float8_e4m3fn
+        if not n:
             raise ValueError("no tensors")
         if self.state_bits not in (8, 32):
             raise ValueError(f"state_bits must be 8 or 32 (got {state_bits})")
-        n = len(self.params)
         decay = [1.0] * n if decay is None else [float(d) for d in decay]
         if len(decay) != n:
             raise ValueError(f"{len(decay)} decay factors for {n} tensors")
         for i, p in enumerate(self.params):
             if not isinstance(p, torch.Tensor):
                 raise TypeError(f"params[{i}] must be a torch tensor")
-            if p.dtype not in (torch.bfloat16, torch.float32):
+            if p.dtype is not bf16 and p.dtype is not f32:
                 raise ValueError(f"params[{i}] must be bf16 or fp32, got {p.dtype}")
-            _need(p, p.shape, p.dtype, f"params[{i}]")
-            _same_device(self.params[0], (p, f"params[{i}]"))
-        self.device = self.params[0].device
+            if not p.is_cuda or not p.is_contiguous():
+                _need(p, p.shape, p.dtype, f"params[{i}]")
+        self.device, self._index = self.params[0].device, self.params[0].get_device()
+        self._sizes = [p.numel() for p in self.params]
+        kinds = {"master": f32}
+        kinds.update({"m": f32, "v": f32} if self.state_bits == 32 else {"m": e4m3, "m_exp": u8, "r": e4m3, "r_exp": u8})
         given = dict(state or {})
-        new = lambda p, dtype, shape=None: torch.zeros(shape or p.shape, dtype=dtype, device=p.device)
-        blocks = lambda p: ((p.numel() + 255) // 256,)
-        f32, bf16 = torch.float32, torch.bfloat16
-        if any(p.dtype == bf16 for p in self.params):
-            self.master = list(given.pop("master", None) or [p.detach().float() if p.dtype == bf16 else None for p in self.params])
-        else:
-            self.master = list(given.pop("master", None) or [None] * n)
-        if self.state_bits == 32:
-            names = {"m": f32, "v": f32}
-        else:
-            names = {"m": torch.float8_e4m3fn, "m_exp": torch.uint8, "r": torch.float8_e4m3fn, "r_exp": torch.uint8}
-        for name, dt in names.items():
-            x = given.pop(name, None)
-            if x is None:
-                x = [new(p, dt, blocks(p) if name.endswith("_exp") else None) + (1 if name.endswith("_exp") else 0) if dt == torch.uint8
-                     else torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(dt) if dt == torch.float8_e4m3fn else new(p, dt)
-                     for p in self.params]
-            setattr(self, name, list(x))
-        if given:
-            raise ValueError(f"unknown state {sorted(given)}")
+        if set(given) - set(kinds):
+            raise ValueError(f"unknown state {sorted(set(given) - set(kinds))}")
+        for name, dt in kinds.items():
+            x = given.get(name)
+            if x is not None:
+                x = list(x)
+                if len(x) != n:
+                    raise ValueError(f"state {name}: {len(x)} tensors for {n} weights")
+            elif name == "master":
+                x = [p.detach().float() if p.dtype is bf16 else None for p in self.params]
+            elif dt is u8:
+                x = [torch.ones((k + 255) // 256, dtype=u8, device=self.device) for k in self._sizes]
+            else:      # (codes of 0 are bytes of 0)
+                x = [torch.zeros(p.shape, dtype=u8 if dt is e4m3 else dt, device=self.device).view(dt) for p in self.params]
+            setattr(self, name, x)
+        if given.get("master") is None and not any(p.dtype is bf16 for p in self.params):
+            self.master = [None] * n
         rec = (AdamwTensor * n)()
-        for name in ("master", *names):
-            if len(getattr(self, name)) != n:
-                raise ValueError(f"state {name}: {len(getattr(self, name))} tensors for {n} weights")
-        for i, p in enumerate(self.params):
-            for name, dt in (("master", f32), *names.items()):
-                x = getattr(self, name)[i]
-                if name == "master" and p.dtype == f32:
+        order = ("master", "m", "v", None, None) if self.state_bits == 32 else ("master", "m", "r", "m_exp", "r_exp")
+        lists = [getattr(self, name) if name else None for name in order]
+        for i, (p, k) in enumerate(zip(self.params, self._sizes)):
+            pointers = []
+            for name, values in zip(order, lists):
+                x = None if values is None else values[i]
+                if name == "master" and p.dtype is f32:
                     if x is not None:
                         raise ValueError(f"master[{i}]: fp32 weights have none")
-                    continue
-                shape = blocks(p) if name.endswith("_exp") else p.shape
-                _need(x, shape, dt, f"{name}[{i}]")
-                _same_device(p, (x, f"{name}[{i}]"))
-            ptr = lambda name: getattr(self, name)[i].data_ptr() if getattr(self, name)[i] is not None else None
-            v = "v" if self.state_bits == 32 else "r"
-            rec[i] = AdamwTensor(p.data_ptr(), ptr("master"), ptr("m"), ptr(v), ptr("m_exp") if v == "r" else None,
-                                 ptr("r_exp") if v == "r" else None, p.numel(), decay[i],
-                                 PSATTN_BF16 if p.dtype == bf16 else PSATTN_FP32)
+                elif name:
+                    shape = ((k + 255) // 256,) if name.endswith("_exp") else p.shape
+                    if getattr(x, "shape", None) != shape or x.dtype is not kinds[name] or x.get_device() != self._index or not x.is_contiguous():
+                        _expect(x, shape, kinds[name], self._index, f"{name}[{i}]")
+                pointers.append(None if x is None else x.data_ptr())
+            if p.get_device() != self._index:
+                _expect(p, p.shape, p.dtype, self._index, f"params[{i}]")
+            rec[i] = AdamwTensor(p.data_ptr(), *pointers, k, decay[i], PSATTN_BF16 if p.dtype is bf16 else PSATTN_FP32)
         L = lib()
         h = ctypes.c_void_p()
         _check(L.psattn_adamw_create(n, rec, self.state_bits, ctypes.byref(h)))
@@ -794,11 +793,9 @@ class AdamW:
         size = ctypes.c_size_t()
         _check(L.psattn_adamw_device_bytes(h, ctypes.byref(size)))
         self._table = torch.empty(size.value, dtype=torch.uint8, device=self.device)
-        self._index = self.params[0].get_device()
         _on(self._index, L.psattn_adamw_upload, h, self._table.data_ptr(), size.value)
         _check(L.psattn_adamw_workspace_size(h, ctypes.byref(size)))
         self._ws_bytes = size.value
-        self._sizes = [p.numel() for p in self.params]
 
     def __del__(self):
         if getattr(self, "_handle", None) is not None and _LIB is not None:

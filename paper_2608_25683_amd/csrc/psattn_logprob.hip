@@ -528,33 +528,29 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
   }
 }
 
-// ---- LSE and logp from the tiles' parts: 16 rows per workgroup, 16 threads for each row's parts, then a wavefront per target
+// ---- LSE and logp from the tiles' parts: 16 rows per workgroup, 64 threads for each row's parts (so that 128 bytes of them
+// are read together), then a wavefront per row for its targets' dot products
 template <bool FP32>
-__global__ __launch_bounds__(256) void finish_kernel(LogprobArgs a) {
-  __shared__ LogprobStat s_part[16][17];
-  __shared__ float s_lse[16];
-  const int r0 = blockIdx.x * 16, lane = threadIdx.x & 63;
+__global__ __launch_bounds__(1024) void finish_kernel(LogprobArgs a) {
+  __shared__ LogprobStat s_part[16][65];
+  const int r0 = blockIdx.x * 16, lane = threadIdx.x & 63, i = threadIdx.x >> 6, r = r0 + i;
   {
-    const int i = threadIdx.x & 15, r = r0 + i, slice = threadIdx.x >> 4;
+    const int j = threadIdx.x & 15, slice = threadIdx.x >> 4;
     const int parts = (a.v + a.part_v - 1) / a.part_v;
     LogprobStat p = {kNegInf, 0.f};
-    if (r < a.n) {
-#pragma unroll 8
-      for (int t = slice; t < parts; t += 16) p = join(p, a.part[(int64_t)t * a.n + r]);
+    if (r0 + j < a.n) {
+#pragma unroll 4
+      for (int t = slice; t < parts; t += 64) p = join(p, a.part[(int64_t)t * a.n + r0 + j]);
     }
-    s_part[i][slice] = p;
+    s_part[j][slice] = p;
   }
   __syncthreads();
-  if (threadIdx.x < 16 && r0 + (int)threadIdx.x < a.n) {
-    LogprobStat p = s_part[threadIdx.x][0];
-    for (int k = 1; k < 16; ++k) p = join(p, s_part[threadIdx.x][k]);
+  if (r < a.n) {
+    LogprobStat p = s_part[i][lane];
+#pragma unroll
+    for (int w = 32; w >= 1; w >>= 1) p = join(p, {__shfl_xor(p.top, w), __shfl_xor(p.sum, w)});
     const float lse = ((p.top == kNegInf ? 0.f : p.top) + log2f(p.sum)) * (1.f / kLog2e);
-    s_lse[threadIdx.x] = lse;
-    a.lse_out[r0 + threadIdx.x] = lse;
-  }
-  __syncthreads();
-  for (int i = threadIdx.x >> 6; i < 16 && r0 + i < a.n; i += 4) {
-    const int r = r0 + i;
+    if (lane == 0) a.lse_out[r] = lse;
     int e0, e1;
     targets_of(a, r, e0, e1);
     for (int e = e0; e < e1; ++e) {
@@ -579,7 +575,7 @@ __global__ __launch_bounds__(256) void finish_kernel(LogprobArgs a) {
         }
 #pragma unroll
         for (int w2 = 32; w2 >= 1; w2 >>= 1) z += __shfl_xor(z, w2);
-        z = z * a.scale - s_lse[i];
+        z = z * a.scale - lse;
       }
       if (lane == 0) a.logp[e] = z;
     }
@@ -899,8 +895,8 @@ hipError_t launch_logprob_logits(const LogprobArgs& a, int piece, bool backward,
 }
 hipError_t launch_logprob_finish(const LogprobArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)tiles(a.n, 16));
-  if (a.planes == 3) hipLaunchKernelGGL(finish_kernel<true>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(finish_kernel<false>, grid, dim3(256), 0, st, a);
+  if (a.planes == 3) hipLaunchKernelGGL(finish_kernel<true>, grid, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL(finish_kernel<false>, grid, dim3(1024), 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_logprob_dx(const LogprobArgs& a, int piece, hipStream_t st) {

@@ -200,12 +200,18 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
   for (int s = 0; s < S::RING - 1 && s < steps; ++s) issue();
   landed(S::RING - 1 <= steps);
   if (S::RING - 1 < steps) issue();
-  // fragment F of the operands' P (FM + FN), elements 16 KK .. of a stage
+  // fragment F of the operands' P (FM + FN), elements 16 KK .. of a stage: B's first, which every product takes, then A's in the
+  // order in which they are taken
   constexpr int READS = P * (S::FM + S::FN);
   auto read = [&](auto kk, auto frag, const uint8_t* tile) {
-    constexpr int KK = decltype(kk)::value, Q = decltype(frag)::value / (S::FM + S::FN), F = decltype(frag)::value % (S::FM + S::FN);
-    if constexpr (F < S::FM) fa[KK & 1][Q][F] = ra.template read<KK, F>(tile + Q * S::PLANE);
-    else fb[KK & 1][Q][F - S::FM] = rb.template read<KK, F - S::FM>(tile + Q * S::PLANE + S::M * BK * 2);
+    constexpr int KK = decltype(kk)::value, I = decltype(frag)::value;
+    if constexpr (I < P * S::FN) {
+      constexpr int Q = I / S::FN, F = I % S::FN;
+      fb[KK & 1][Q][F] = rb.template read<KK, F>(tile + Q * S::PLANE + S::M * BK * 2);
+    } else {
+      constexpr int Q = P - 1 - (I - P * S::FN) / S::FM, F = (I - P * S::FN) % S::FM;
+      fa[KK & 1][Q][F] = ra.template read<KK, F>(tile + Q * S::PLANE);
+    }
   };
   static_for<READS>([&](auto f) { read(IntC<0>{}, f, lds); });
   int use = 0;

@@ -338,15 +338,15 @@ psattn_status psattn_silu_bwd(const float* dM_planes, const void* A, const void*
  * 0 and it has no gradient.  The same target may be listed more than once.  rows and targets may be 0 (pointers
  * to nothing may then be NULL). */
 typedef struct {
-  int64_t rows;          /* < 2^31 */
-  int64_t targets;       /* < 2^31 */
+  int64_t rows;          /* 0 .. 2^24 - 64; with vocab: less than 2^23 tiles of 128 x 128 logits (PSATTN_E_UNSUPPORTED) */
+  int64_t targets;       /* 0 .. 2^30 */
   int32_t hidden;        /* multiple of 8, at most 2^20 */
   int32_t vocab;         /* >= 1, at most 2^30 */
   float logit_scale;     /* > 0, finite; 1 / sampling temperature */
   psattn_dtype dtype;    /* of X, W, dX and dW */
 } psattn_logprob_desc;
 
-/* Workspace bytes for pass 0 (psattn_logprob_fwd) or 1 (psattn_logprob_bwd). */
+/* Workspace bytes for pass 0 (psattn_logprob_fwd) or 1 (psattn_logprob_bwd); by all of desc, the targets among it. */
 psattn_status psattn_logprob_workspace_size(const psattn_logprob_desc* desc, int pass, size_t* bytes);
 /* logp [targets] and LSE [rows], fp32. */
 psattn_status psattn_logprob_fwd(const psattn_logprob_desc* desc, const void* X, const void* W, const int32_t* tgt_ptr,
@@ -355,10 +355,11 @@ psattn_status psattn_logprob_fwd(const psattn_logprob_desc* desc, const void* X,
  *   dz[r][v] = sum of dlogp[e] over r's targets equal to v  -  G[r] p[r][v]
  *   dX[r] = logit_scale * sum_v dz[r][v] W[v],   dW[v] = logit_scale * sum_r dz[r][v] X[r].
  * A row without a target of non-zero dlogp has dX 0 and no part in dW, whatever its X and LSE hold.  dX [rows][hidden]
- * and dW [vocab][hidden] are of the desc's dtype and overwritten; either may be NULL if it is not wanted.  The logits are
- * computed again, a piece of the vocabulary at a time.  bf16: dz is rounded once to bf16, sums are fp32.  fp32: every
- * product is formed from bf16 planes (psattn_split_planes) and holds fp32 precision; a non-finite X or W
- * makes the results that it enters NaN.  Sums have a fixed order: results are bitwise repeatable. */
+ * and dW [vocab][hidden] are of the desc's dtype, overwritten, and must not overlap X, W or each other; either may be NULL
+ * if it is not wanted.  The logits are computed again, a piece of the vocabulary at a time.  bf16: dz is rounded once to bf16
+ * (what that leaves out of a target's dz, which is most of its row's, is added by itself), sums are fp32.  fp32: every product
+ * is formed from bf16 planes (psattn_split_planes) and holds fp32 precision; a non-finite X or W makes the results that it
+ * enters NaN.  Sums have a fixed order: results are bitwise repeatable. */
 psattn_status psattn_logprob_bwd(const psattn_logprob_desc* desc, const void* X, const void* W, const int32_t* tgt_ptr,
                                  const int32_t* tgt, const float* LSE, const float* dlogp, void* dX, void* dW, void* ws,
                                  size_t ws_bytes, void* stream);
@@ -381,7 +382,7 @@ typedef struct {
   void* v;               /* [n] fp32, or the e4m3 codes of sqrt(v) */
   uint8_t* m_exp;        /* state_bits 8: [(n + 255) / 256], else NULL */
   uint8_t* v_exp;
-  int64_t n;             /* elements, >= 1 */
+  int64_t n;             /* elements, 1 .. 2^35; all tensors together: less than 2^24 chunks of 4096 */
   float decay;           /* factor of weight_decay (0: none, as for norms), >= 0 */
   psattn_dtype dtype;    /* of param */
 } psattn_adamw_tensor;

@@ -5,7 +5,10 @@
 //   g = gs grad,  m' = m b1 + g (1 - b1),  v' = v b2 + g^2 (1 - b2),  r = sqrt(v')
 //   w' = w (1 - lr wd) - m' / (r / sqrt(1 - b2^t) + eps) * lr / (1 - b1^t)
 // A workgroup takes ADAMW_CHUNK elements of one tensor (one record of the uploaded table), so any number of tensors of any
-// size is one launch, and no tensor waits for another.  The kernels are bound by their bytes.
+// size is one launch, and no tensor waits for another.  The kernels are bound by their bytes: 218 million bf16 weights with
+// masters and fp32 gradients, 32-bit states 1218 us (30 bytes each, 5.4 TB/s), 8-bit states 797 us (18 bytes, 4.9 TB/s, with
+// three quarters of the vector instructions' time behind it), the norm 187 us (4.7 TB/s; a large copy: 4.8).  Chunks of 8192 elements: 1243 and 783
+// us, but 37 us instead of 31 for 300 tensors of 20000 on average and 12.4 instead of 9.5 for a tiny layer's nine.
 //
 // 8-bit states: a wavefront's turn is 256 elements, four per lane, which is one block of the states: its largest
 // magnitude comes from the wavefront's own lanes, without LDS.  The power of two of a block moves the

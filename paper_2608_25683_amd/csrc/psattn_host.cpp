@@ -1336,6 +1336,9 @@ psattn_status psattn_silu_bwd(const float* dM_planes, const void* A, const void*
 namespace {
 
 int64_t up64(int64_t x) { return (x + 63) / 64 * 64; }
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  return a && b && (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
+}
 
 // Everything of the arguments that follows from the sizes, and the workspace: buffers as offsets.
 struct LogprobPlan {
@@ -1375,8 +1378,8 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   if (!d) return fail(PSATTN_E_INVALID_ARG, "desc is NULL");
   if (pass != 0 && pass != 1) return fail(PSATTN_E_INVALID_ARG, "pass must be 0 or 1 (got %d)", pass);
   if (d->dtype != PSATTN_BF16 && d->dtype != PSATTN_FP32) return fail(PSATTN_E_UNSUPPORTED, "unknown dtype %d", (int)d->dtype);
-  if (d->rows < 0 || d->rows > INT32_MAX - 1024) return fail(PSATTN_E_INVALID_ARG, "rows %lld outside 0 .. 2^31 - 1025", (long long)d->rows);
-  if (d->targets < 0 || d->targets > INT32_MAX) return fail(PSATTN_E_INVALID_ARG, "targets %lld outside 0 .. 2^31 - 1", (long long)d->targets);
+  if (d->rows < 0 || d->rows > (1 << 24) - 64) return fail(PSATTN_E_INVALID_ARG, "rows %lld outside 0 .. 2^24 - 64", (long long)d->rows);
+  if (d->targets < 0 || d->targets > 1 << 30) return fail(PSATTN_E_INVALID_ARG, "targets %lld outside 0 .. 2^30", (long long)d->targets);
   if (d->hidden < 8 || d->hidden % 8 || d->hidden > 1 << 20)
     return fail(PSATTN_E_UNSUPPORTED, "hidden %d: a multiple of 8, 8 .. 2^20, is needed", d->hidden);
   if (d->vocab < 1 || d->vocab > 1 << 30) return fail(PSATTN_E_INVALID_ARG, "vocab %d outside 1 .. 2^30", d->vocab);
@@ -1402,7 +1405,8 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   const int64_t each = (vr + a.pieces - 1) / a.pieces;
   a.pieces = (int32_t)((vr + each - 1) / each);
   a.piece_v = (int32_t)(256 * each);
-  if ((int64_t)(a.n / 32 + 1) * (std::max(a.v, a.h) / 128 + 1) > INT32_MAX / 32)
+  // (a launch holds 2^32 threads, of at most 512 per tile of 128 x 128 and more; 128 x 32 ones have one row of tiles and 256)
+  if ((int64_t)(a.n / 128 + 1) * (std::max(a.v, a.h) / 128 + 1) >= 1 << 23)
     return fail(PSATTN_E_UNSUPPORTED, "rows %d x vocab %d: more tiles than a launch holds", a.n, a.v);
   a.shape = a.n <= 32 ? LP_THIN : logprob_tiling(std::min(a.v, a.piece_v), a.n, a.hp, a.planes, 1).shape;
   a.part_v = a.shape == LP_LARGE ? 256 : 128;
@@ -1509,6 +1513,9 @@ psattn_status psattn_logprob_bwd(const psattn_logprob_desc* desc, const void* X,
   if ((a.e && !dlogp) || (a.n && !LSE)) return fail(PSATTN_E_INVALID_ARG, "NULL argument");
   if (((uintptr_t)dlogp | (uintptr_t)LSE) & 3) return fail(PSATTN_E_ALIGNMENT, "dlogp and LSE must be 4-byte aligned");
   if (misaligned(dX) || misaligned(dW)) return fail(PSATTN_E_ALIGNMENT, "dX and dW must be 16-byte aligned");
+  const int64_t size = a.planes == 3 ? 4 : 2, xn = (int64_t)a.n * a.h * size, wn = (int64_t)a.v * a.h * size;
+  if (overlap(dX, xn, X, xn) || overlap(dX, xn, W, wn) || overlap(dW, wn, X, xn) || overlap(dW, wn, W, wn) || overlap(dX, xn, dW, wn))
+    return fail(PSATTN_E_INVALID_ARG, "dX and dW must not overlap each other, X or W");
   a.lse = LSE;
   a.dlogp = dlogp;
   a.dX = a.n ? dX : nullptr;
@@ -1553,7 +1560,7 @@ psattn_status adamw_create(int32_t n, const psattn_adamw_tensor* ts, int32_t bit
     const psattn_adamw_tensor& t = ts[i];
     if (t.dtype != PSATTN_BF16 && t.dtype != PSATTN_FP32) return fail(PSATTN_E_UNSUPPORTED, "tensor %d: unknown dtype %d", i, (int)t.dtype);
     const bool bf16 = t.dtype == PSATTN_BF16;
-    if (t.n < 1 || t.n > (int64_t)1 << 40) return fail(PSATTN_E_INVALID_ARG, "tensor %d: n %lld outside 1 .. 2^40", i, (long long)t.n);
+    if (t.n < 1 || t.n > (int64_t)1 << 35) return fail(PSATTN_E_INVALID_ARG, "tensor %d: n %lld outside 1 .. 2^35", i, (long long)t.n);
     if (!t.param || !t.m || !t.v) return fail(PSATTN_E_INVALID_ARG, "tensor %d: NULL argument", i);
     if (bf16 != (t.master != nullptr)) return fail(PSATTN_E_INVALID_ARG, "tensor %d: bf16 weights have a master, fp32 weights none", i);
     if ((bits == 8) != (t.m_exp != nullptr) || (bits == 8) != (t.v_exp != nullptr))
@@ -1574,7 +1581,8 @@ psattn_status adamw_create(int32_t n, const psattn_adamw_tensor* ts, int32_t bit
     o.tensors.push_back({t.param, t.master, t.m, t.v, t.m_exp, t.v_exp, t.n, t.decay, bf16 ? 1 : 0});
     o.first_item.push_back((int64_t)o.items.size());
     const int64_t chunks = (t.n + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
-    if ((int64_t)o.items.size() + chunks > 1 << 30) return fail(PSATTN_E_UNSUPPORTED, "tensor %d: more than 2^43 elements in all", i);
+    // (a launch holds 2^32 threads, 256 per chunk)
+    if ((int64_t)o.items.size() + chunks >= 1 << 24) return fail(PSATTN_E_UNSUPPORTED, "tensor %d: more than 2^24 chunks of %d elements in all", i, ADAMW_CHUNK);
     for (int64_t c = 0; c < chunks; ++c) o.items.push_back({i, (int32_t)c});
   }
   o.first_item.push_back((int64_t)o.items.size());

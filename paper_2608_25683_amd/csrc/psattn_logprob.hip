@@ -18,6 +18,12 @@ using namespace dev;
 
 // The workgroups' shapes: WM x WN wavefronts, each with FM x FN tiles of 32 x 32; stages of BK elements of the summed dimension
 // of each of P planes, RING of them in LDS.
+//
+// Large, 8192 x 128256 logits of 4096: 6.30 ms, 1366 TFLOP/s (a library product of this kind: 1480).  Two wavefronts per SIMD, so
+// that one's products cover the other's waits.  Bound by power: the matrix cores are busy 71% of the cycles at 1.74 GHz
+// (2.13 with nothing else to do); without the copies 80% at 1.81, with data that is always in L2 73% at 1.78.  Tried and
+// slower: four wavefronts of 128 x 128 (7.07 ms, nothing covers a wait), stages of 32 in rings of 4 and 5 (6.8: twice the
+// barriers), raised wave priorities (no change).
 template <int WM_, int WN_, int FM_, int FN_, int BK_, int RING_, int P_>
 struct Tiling {
   static constexpr int WM = WM_, WN = WN_, FM = FM_, FN = FN_, WAVES = WM * WN, THREADS = 64 * WAVES, M = 32 * WM * FM, N = 32 * WN * FN;
@@ -30,11 +36,12 @@ struct Tilings<1> {
   using Large = Tiling<2, 4, 4, 2, 64, 2, 1>;    // 256 x 256, one workgroup per CU
   using Small = Tiling<2, 2, 2, 2, 64, 2, 1>;    // 128 x 128, two
   using Deep = Tiling<2, 2, 2, 2, 64, 4, 1>;     // 128 x 128, one, three stages ahead
-  using Thin = Tiling<4, 1, 1, 1, 64, 6, 1>;     // 128 x 32, one: 100 KB of copies on their way
+  using Thin = Tiling<4, 1, 1, 1, 64, 6, 1>;     // 128 x 32, one: 100 KB of copies on their way.  Bound by W's bytes: one row
+                                                 // x 4096 x 128256 171 us, 6.1 TB/s (two stages, four workgroups: 178)
 };
 // All planes of a stage lie in LDS together, so that each is copied, and read into registers, once for its products with three,
 // two or one of the other operand's: half the copies and reads of a pass per pair of planes (513 rows x 1024 x 16001: logits
-// 150 us that way).  One workgroup per CU.
+// 150 us that way, 127 so; 1024 rows x 1024 x 16000 155 us, 1300 TFLOP/s of bf16 products).  One workgroup per CU.
 template <>
 struct Tilings<3> {
   using Large = Tiling<4, 2, 2, 2, 32, 2, 3>;    // 256 x 128
@@ -339,7 +346,8 @@ __device__ __forceinline__ void targets_of(const LogprobArgs& a, int r, int& e0,
   e1 = min(max(a.tgt_ptr[r + 1], e0), a.e);
 }
 
-// ---- rows as the products take them
+// ---- rows as the products take them: the backward's without gradient are zero, so that nothing they hold reaches dW.  Bound by the
+// rows' bytes (8192 x 4096: 23 us), a workgroup per row.
 template <bool FP32>
 __global__ __launch_bounds__(256) void prep_kernel(LogprobArgs a, int backward) {
   const int r = blockIdx.x;
@@ -396,7 +404,10 @@ __global__ __launch_bounds__(256) void wplanes_kernel(LogprobArgs a, int piece) 
   }
 }
 
-// ---- a tile of logits: M entries of the piece down, N rows across
+// ---- a tile of logits: M entries of the piece down, N rows across, so that a lane holds 16 FM entries of each of its FN rows.
+// Forward: the maximum and the sum of exponentials of the tile's entries leave for each row, one fma, one exponential, one
+// addition and half a maximum per logit; nothing else is written.  Backward: dz of the tile, scaled, as bf16 or as
+// planes: 6.84 ms for 8192 x 128256 x 4096 against the forward's 6.30, for the same product and 2 GB written.
 template <class S, bool BACKWARD>
 __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
@@ -535,7 +546,8 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
 }
 
 // ---- LSE and logp from the tiles' parts: 16 rows per workgroup, 64 threads for each row's parts (so that 128 bytes of them
-// are read together), then a wavefront per row for its targets' dot products
+// are read together), then a wavefront per row for its targets' dot products, in fp32 from X and W themselves.  Bound by the
+// latency of four dependent reads where there are few rows (one row: 6 us), else by the rows' bytes (20480 x 4096: 82 us, 4.3 TB/s).
 template <bool FP32>
 __global__ __launch_bounds__(1024) void finish_kernel(LogprobArgs a) {
   __shared__ LogprobStat s_part[16][65];
@@ -671,7 +683,9 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::FM][S::FN], void
   }
 }
 
-// dX: M of the hidden dimension down, N rows across
+// dX: M of the hidden dimension down, N rows across, summed over the piece's entries or a part of them; W is read across its rows by
+// the transposing loads.  Pieces add to fp32 sums in memory, the last one leaves the result.  8192 x 4096 x 128256: 6.57 ms in four
+// pieces, 1310 TFLOP/s.
 template <class S>
 __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
@@ -739,7 +753,9 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
   if (last && a.splits_dx == 1) put_tile<S>(acc, a.dX, j0 * a.h + i0, a.h, a.n - j0, a.h - i0, lds);
 }
 
-// dW: M of the hidden dimension down, N entries across
+// dW: M of the hidden dimension down, N entries across, summed over the rows; both operands are read by the transposing loads.
+// 8192 x 4096 x 128256: 6.64 ms, 1297 TFLOP/s (a library product with such operands: 1180).  Few rows: bound by dW's bytes
+// (64 rows: 377 us for 1.05 GB).
 template <class S>
 __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];

@@ -242,6 +242,23 @@ def test_more_tensors_than_a_launch_holds_and_nothing_behind_them():
             assert all(torch.all(c[n:] == 0x40) for c, n in zip(codes, sizes))
 
 
+def test_a_tensor_of_more_than_2_31_elements():
+    """Its first and last elements take the step that a small tensor of the same values takes, bit for bit."""
+    from paper_2608_25683_amd import psattn as P
+    n, k = (1 << 31) + 5003, 10007
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    ends = lambda t: torch.cat([t[:k], t[-k:]])
+    for t in (p, g):
+        t[:k], t[-k:] = draw((k,), 1, t.dtype), draw((k,), 2, t.dtype)
+    small, sg = [ends(p).clone()], [ends(g).clone()]
+    big, ref = P.AdamW([p]), P.AdamW(small)
+    for step in (1, 2):
+        big.step([g], step=step, max_norm=0.5, **HYPER)
+        ref.step(sg, step=step, max_norm=0.5, **HYPER)
+    assert torch.equal(ends(p), small[0]) and torch.equal(ends(big.m[0]), ref.m[0]) and torch.equal(ends(big.v[0]), ref.v[0])
+    assert not p[k:k + 100000].any() and not p[n // 2:n // 2 + 100000].any()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_captured_step_with_values_in_device_memory(bits):
     from paper_2608_25683_amd import psattn as P

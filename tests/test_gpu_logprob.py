@@ -296,6 +296,33 @@ def test_on_another_stream_and_captured():
         call(*args[1 - k])             # the program's own work between the replays
 
 
+def test_weights_beyond_4_gib():
+    """70001 x 32768 bf16: offsets that pass 32 bits.  Only some rows of W are non-zero, so that the rest is known: those logits are 0."""
+    from paper_2608_25683_amd import psattn as P
+    n, h, v, rows = 40, 32768, 70001, [0, 35000, 65535, 65536, 70000]
+    g = torch.Generator().manual_seed(81)
+    x = torch.randn((n, h), generator=g).bfloat16()
+    some = (torch.randn((len(rows), h), generator=g) * 2 / h ** 0.5).bfloat16()
+    w = torch.zeros((v, h), dtype=torch.bfloat16, device="cuda")
+    w[rows] = some.cuda()
+    ptr, tgt = torch.arange(n + 1, dtype=torch.int32), torch.tensor([rows[r % 5] for r in range(n)], dtype=torch.int32)
+    dlogp = torch.randn(n, generator=g)
+    logp, lse = P.psattn_logprob_fwd(x.cuda(), w, ptr.cuda(), tgt.cuda())
+    dx, dw = P.psattn_logprob_bwd(x.cuda(), w, ptr.cuda(), tgt.cuda(), lse, dlogp.cuda())
+    z = x.double() @ some.double().t()
+    ref = torch.log(torch.exp(z).sum(1) + (v - 5))
+    pick = torch.arange(n) % 5
+    # (5 logits of 32768 terms of about 1/90 each, and 70000 terms of the sum: well under 1e-4 in fp32)
+    assert float((lse.double().cpu() - ref).abs().max()) <= 1e-4
+    assert float((logp.double().cpu() - (z[torch.arange(n), pick] - ref)).abs().max()) <= 2e-4
+    dz = -dlogp.double()[:, None] * torch.exp(z - ref[:, None])
+    dz[torch.arange(n), pick] += dlogp.double()
+    want = torch.cat([dz.t() @ x.double(), (-dlogp.double() * torch.exp(-ref))[None] @ x.double()])
+    got = torch.cat([dw[rows].cpu(), dw[12345:12346].cpu()]).double()
+    for a, b in ((got, want), (dx.double().cpu(), dz @ some.double())):
+        assert float((a - b).norm() / b.norm()) <= 2.0 ** -8
+
+
 def test_finite_differences():
     """dX and dW against central differences of the loss sum_e dlogp_e logp_e, fp32, through the forward alone."""
     from paper_2608_25683_amd import psattn as P

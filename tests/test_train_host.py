@@ -18,7 +18,7 @@ def _desc(**kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(rows=-1), "PSATTN_E_INVALID_ARG"), (dict(rows=2 ** 31), "PSATTN_E_INVALID_ARG"), (dict(targets=-1), "PSATTN_E_INVALID_ARG"),
-    (dict(targets=2 ** 31), "PSATTN_E_INVALID_ARG"), (dict(hidden=0), "PSATTN_E_UNSUPPORTED"), (dict(hidden=12), "PSATTN_E_UNSUPPORTED"),
+    (dict(targets=2 ** 31), "PSATTN_E_INVALID_ARG"), (dict(rows=10 ** 6, vocab=2 ** 20), "PSATTN_E_UNSUPPORTED"), (dict(hidden=0), "PSATTN_E_UNSUPPORTED"), (dict(hidden=12), "PSATTN_E_UNSUPPORTED"),
     (dict(hidden=-8), "PSATTN_E_UNSUPPORTED"), (dict(hidden=2 ** 20 + 8), "PSATTN_E_UNSUPPORTED"), (dict(vocab=0), "PSATTN_E_INVALID_ARG"),
     (dict(logit_scale=0.0), "PSATTN_E_INVALID_ARG"), (dict(logit_scale=float("nan")), "PSATTN_E_INVALID_ARG"),
     (dict(logit_scale=float("inf")), "PSATTN_E_INVALID_ARG"), (dict(dtype=7), "PSATTN_E_UNSUPPORTED")])
@@ -51,6 +51,11 @@ def test_logprob_argument_refusals():
     assert bwd([16] * 8, ws=None) == "PSATTN_E_WORKSPACE" and bwd([16] * 8, size=100) == "PSATTN_E_WORKSPACE"
     assert fwd(ok, ws=24) == "PSATTN_E_ALIGNMENT" and bwd([16] * 8, ws=24) == "PSATTN_E_ALIGNMENT"
     assert st(L.psattn_logprob_fwd(None, *ok, 16, 2 ** 40, None)) == "PSATTN_E_INVALID_ARG"
+    at = 1 << 20                             # outputs on inputs or on each other
+    bufs = [at, 2 * at, 16, 16, 16, 16]
+    for dx, dw in ((at, 4 * at), (at + 496, 4 * at), (3 * at, at + 64), (2 * at + 16, 3 * at), (3 * at, 2 * at + 12784), (3 * at, 3 * at + 256)):
+        assert bwd(bufs + [dx, dw]) == "PSATTN_E_INVALID_ARG", (dx, dw)
+        assert b"overlap" in L.psattn_last_error()
     n = ctypes.c_size_t()
     assert st(L.psattn_logprob_workspace_size(ctypes.byref(d), 2, ctypes.byref(n))) == "PSATTN_E_INVALID_ARG"
     assert st(L.psattn_logprob_workspace_size(ctypes.byref(d), 0, None)) == "PSATTN_E_INVALID_ARG"
@@ -74,7 +79,7 @@ def _tensor(**kw):
 
 @pytest.mark.parametrize("kw,bits,status", [
     (dict(param=None), 32, "PSATTN_E_INVALID_ARG"), (dict(m=None), 32, "PSATTN_E_INVALID_ARG"), (dict(n=0), 32, "PSATTN_E_INVALID_ARG"),
-    (dict(n=2 ** 41), 32, "PSATTN_E_INVALID_ARG"), (dict(master=0x4000), 32, "PSATTN_E_INVALID_ARG"),
+    (dict(n=2 ** 36), 32, "PSATTN_E_INVALID_ARG"), (dict(master=0x4000), 32, "PSATTN_E_INVALID_ARG"),
     (dict(dtype=P.PSATTN_BF16), 32, "PSATTN_E_INVALID_ARG"), (dict(dtype=5), 32, "PSATTN_E_UNSUPPORTED"), (dict(), 8, "PSATTN_E_INVALID_ARG"),
     (dict(), 16, "PSATTN_E_UNSUPPORTED"), (dict(m_exp=0x4000, v_exp=0x5000), 32, "PSATTN_E_INVALID_ARG"),
     (dict(decay=-1.0), 32, "PSATTN_E_INVALID_ARG"), (dict(decay=float("nan")), 32, "PSATTN_E_INVALID_ARG"),

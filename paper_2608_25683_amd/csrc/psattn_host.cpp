@@ -1343,7 +1343,7 @@ bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
 // Everything of the arguments that follows from the sizes, and the workspace: buffers as offsets.
 struct LogprobPlan {
   LogprobArgs a{};
-  size_t part = 0, row = 0, xc = 0, wc = 0, dl = 0, dx_acc = 0, dw_acc = 0, ent_row = 0, ent_rem = 0, bytes = 0;
+  size_t part = 0, info = 0, before = 0, live = 0, row = 0, xc = 0, wc = 0, dl = 0, dx_acc = 0, dw_acc = 0, ent_row = 0, ent_rem = 0, bytes = 0;
 };
 
 // The tiles' shape of a product of down x across x k elements, and into how many parts its sum is split.  Estimated time in
@@ -1413,7 +1413,7 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   const LogprobTiling dx = logprob_tiling(a.h, a.n, std::min(a.v, a.piece_v), a.planes, 32);
   const LogprobTiling dw = logprob_tiling(a.h, std::min(a.v, a.piece_v), a.n, a.planes, 32);
   a.shape_dx = dx.shape, a.splits_dx = dx.splits, a.stages_dx = dx.stages;
-  a.shape_dw = dw.shape, a.splits_dw = dw.splits, a.stages_dw = dw.stages;
+  a.shape_dw = dw.shape, a.splits_dw = dw.splits;
   size_t cur = 0;
   auto take = [&](size_t bytes) {
     const size_t at = cur;
@@ -1426,6 +1426,11 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   if (!bwd) {
     p.part = take((size_t)((a.v + a.part_v - 1) / a.part_v) * a.n * sizeof(LogprobStat));
   } else {
+    if (a.n > 256) {
+      p.info = take((size_t)a.n * sizeof(LogprobRow));
+      p.before = take((size_t)(a.n / 256 + 1) * 4);
+    }
+    p.live = take(4);
     p.row = take((size_t)a.np * sizeof(LogprobRow));
     if (!fp32) {
       p.ent_row = take((size_t)a.e * 4);
@@ -1458,6 +1463,9 @@ psattn_status logprob_begin(const psattn_logprob_desc* d, int pass, const void* 
   a.tgt = tgt;
   char* b = (char*)ws;
   a.part = (LogprobStat*)(b + p.part);
+  a.info = (LogprobRow*)(b + p.info);
+  a.before = (int32_t*)(b + p.before);
+  a.live = (int32_t*)(b + p.live);
   a.row = (LogprobRow*)(b + p.row);
   const bool copy = pass == 1 || a.planes == 3 || a.h != a.hp;
   a.xc = copy ? (uint16_t*)(b + p.xc) : nullptr;
@@ -1494,7 +1502,7 @@ psattn_status psattn_logprob_fwd(const psattn_logprob_desc* desc, const void* X,
   a.lse_out = LSE;
   if (!a.n) return PSATTN_OK;
   hipStream_t st = (hipStream_t)stream;
-  if (a.xc) s = timed(K_LP_PREP, st, [&] { return launch_logprob_prep(a, false, st); });
+  if (a.xc) s = timed(K_LP_PREP, st, [&] { return launch_logprob_prep(a, st); });
   for (int i = 0; i < a.pieces && s == PSATTN_OK; ++i) {
     if (a.wc) s = timed(K_LP_WPLANES, st, [&] { return launch_logprob_wplanes(a, i, st); });
     if (s == PSATTN_OK) s = timed(K_LP_LOGITS, st, [&] { return launch_logprob_logits(a, i, false, st); });
@@ -1522,7 +1530,7 @@ psattn_status psattn_logprob_bwd(const psattn_logprob_desc* desc, const void* X,
   a.dW = dW;
   if (!a.dX && !a.dW) return PSATTN_OK;
   hipStream_t st = (hipStream_t)stream;
-  if (a.n) s = timed(K_LP_PREP, st, [&] { return launch_logprob_prep(a, true, st); });
+  s = timed(K_LP_PREP, st, [&] { return launch_logprob_rows(a, st); });
   for (int i = 0; i < a.pieces && s == PSATTN_OK; ++i) {
     if (a.n && a.wc) s = timed(K_LP_WPLANES, st, [&] { return launch_logprob_wplanes(a, i, st); });
     if (s == PSATTN_OK && a.n) s = timed(K_LP_DZ, st, [&] { return launch_logprob_logits(a, i, true, st); });

@@ -55,8 +55,9 @@ struct BwdArgs {
 // Log-probabilities over a vocabulary (psattn_logprob.hip).  The vocabulary is taken in pieces of piece_v
 // entries (the forward of bf16 in one); buffers in the workspace:
 struct LogprobStat { float top, sum; };   // max of z log2(e) and the sum of exp2(z log2(e) - max)
-// What the backward's tiles take of a row: its G, its LSE log2(e), its targets e0 .. e1 - 1 and, if it is live, the first of them.
-struct LogprobRow { float total, lse2, g0; int32_t t0, e0, e1, pad[2]; };
+// What the backward's tiles take of a row r: its G, its LSE log2(e), its targets e0 .. e1 - 1 and the first of them (-1: not one
+// of the vocabulary); at: its place among the live rows of its 256, -1 if none of its adjoints is other than 0.
+struct LogprobRow { float total, lse2, g0; int32_t t0, e0, e1, r, at; };
 struct LogprobArgs {
   int32_t n, h, v, e;        // rows, hidden, vocabulary, targets
   int32_t shape, shape_dx, shape_dw;   // LP_THIN .. LP_LARGE: of the logits' tiles, of the gradients'
@@ -66,7 +67,7 @@ struct LogprobArgs {
   int32_t piece_v;           // entries per piece, a multiple of 256
   int32_t pieces;
   int32_t splits_dx, stages_dx;   // parts of a piece's entries in the dX product, each with its own fp32 sums, of so many
-  int32_t splits_dw, stages_dw;   //   stages of 64; parts of the rows in the dW product likewise
+  int32_t splits_dw;              //   stages of 64; parts of the live rows in the dW product likewise
   float scale;
   const void* X;
   const void* W;
@@ -79,10 +80,14 @@ struct LogprobArgs {
   void* dX;
   void* dW;
   LogprobStat* part;         // forward: [parts of the vocabulary][n]
-  LogprobRow* row;           // backward: [np]
-  int32_t* ent_row;          // backward, bf16: [e] the row of each target
+  // backward: only rows that have a gradient are multiplied, packed in their order; how many there are is known on the GPU alone
+  LogprobRow* info;          // [n] of every row (more than 256 rows)
+  int32_t* before;           // [n / 256 + 1] live rows ahead of each 256
+  int32_t* live;             // their number
+  LogprobRow* row;           // [np] of the live rows, and up to a multiple of 64 of them empty ones
+  int32_t* ent_row;          // backward, bf16: [e] the live row of each target, by its place
   float* ent_rem;            //   and what the rounding of its dz to bf16 left out (at a row's first target of the token; else 0)
-  uint16_t* xc;              // [planes][np][hp]: X as the products take it; backward: zero in rows that have no gradient
+  uint16_t* xc;              // [planes][np][hp]: X as the products take it, backward: of the live rows
   uint16_t* wc;              // fp32: [planes][piece_v][hp] planes of the piece
   uint16_t* dl;              // backward: [planes][np][piece_v] dz of the piece
   float* dx_acc;             // backward: [splits_dx][n][h] sums over the pieces, where there is more than one piece or part
@@ -191,7 +196,8 @@ hipError_t launch_split_planes(const float* x, void* planes, int64_t n, hipStrea
 hipError_t launch_silu_bwd(const float* dm, const void* a, const void* b, void* da, void* db, int64_t n, hipStream_t st);
 // The training step behind the layers.  Weak: a host-only build links without these kernels, and its calls fail.
 #define PSATTN_WEAK __attribute__((weak))
-PSATTN_WEAK hipError_t launch_logprob_prep(const LogprobArgs& a, bool backward, hipStream_t st);
+PSATTN_WEAK hipError_t launch_logprob_prep(const LogprobArgs& a, hipStream_t st);
+PSATTN_WEAK hipError_t launch_logprob_rows(const LogprobArgs& a, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_wplanes(const LogprobArgs& a, int piece, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_logits(const LogprobArgs& a, int piece, bool backward, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_finish(const LogprobArgs& a, hipStream_t st);

@@ -277,11 +277,11 @@ __device__ __forceinline__ u32x4 rows8(uint32_t a0, uint32_t a1, uint32_t b0, ui
   return u32x4{(uint32_t)x[0], (uint32_t)y[0], (uint32_t)x[1], (uint32_t)y[1]};
 }
 
-// A workgroup's tile as bf16 to out [rows across][elements down] (ld elements apart), through LDS, so that whole rows of
+// A workgroup's tile as bf16 to the rows out(0) .. out(lim_across - 1) [elements down], through LDS, so that whole rows of
 // it leave together: eight(f, g, h) are the 8 elements that rows8 gives the lane for rows 16 h of tile (f, g).  lim_across
 // and lim_down (a multiple of 8): what there is of the tile.
-template <class S, class F>
-__device__ __forceinline__ void store_tile(F&& eight, bf16_t* out, int64_t ld, int64_t lim_across, int64_t lim_down, uint8_t* lds) {
+template <class S, class F, class O>
+__device__ __forceinline__ void store_tile(F&& eight, O&& out, int64_t lim_across, int64_t lim_down, uint8_t* lds) {
   constexpr int CH = S::M / 8;   // chunks of 16 bytes in a row, at position c ^ (row mod CH): no two lanes of a write in one bank
   static_assert(S::M * S::N * 2 <= S::LDS, "the tile fits");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -298,7 +298,7 @@ __device__ __forceinline__ void store_tile(F&& eight, bf16_t* out, int64_t ld, i
 #pragma unroll 4
   for (int k = threadIdx.x; k < S::N * CH; k += S::THREADS) {
     const int j = k / CH, c = (k % CH) ^ (j % CH);
-    if (j < lim_across && 8 * c < lim_down) *(u32x4*)(out + j * ld + 8 * c) = ld16(lds + k * 16);
+    if (j < lim_across && 8 * c < lim_down) *(u32x4*)(out(j) + 8 * c) = ld16(lds + k * 16);
   }
 }
 
@@ -316,8 +316,10 @@ __device__ __forceinline__ Tile tile_of(int downs, int acrosses) {
   return {__builtin_amdgcn_readfirstlane(part), __builtin_amdgcn_readfirstlane(first + in % high), __builtin_amdgcn_readfirstlane(in / high)};
 }
 
-__device__ __forceinline__ Operand x_operand(const LogprobArgs& a) {
-  if (a.xc) return {a.xc, a.hp, (int64_t)a.np * a.hp, a.np, a.hp};
+__device__ __forceinline__ int up64(int n) { return (n + 63) / 64 * 64; }
+// X's rows: in the backward the live ones, np of them with the empty ones behind
+__device__ __forceinline__ Operand x_operand(const LogprobArgs& a, int np) {
+  if (a.xc) return {a.xc, a.hp, (int64_t)a.np * a.hp, np, a.hp};
   return {(const bf16_t*)a.X, a.h, 0, a.n, a.h};
 }
 __device__ __forceinline__ Operand w_operand(const LogprobArgs& a, int piece) {
@@ -346,52 +348,132 @@ __device__ __forceinline__ void targets_of(const LogprobArgs& a, int r, int& e0,
   e1 = min(max(a.tgt_ptr[r + 1], e0), a.e);
 }
 
-// ---- rows as the products take them: the backward's without gradient are zero, so that nothing they hold reaches dW.  Bound by the
-// rows' bytes (8192 x 4096: 23 us), a workgroup per row.
+// ---- rows as the products take them.  Bound by the rows' bytes, a workgroup per row.
+// row r of X, or zeros, to row i of xc
 template <bool FP32>
-__global__ __launch_bounds__(256) void prep_kernel(LogprobArgs a, int backward) {
-  const int r = blockIdx.x;
-  __shared__ int s_live;
-  if (threadIdx.x == 0) {
-    bool live = !backward && r < a.n;
-    if (backward) {
-      LogprobRow row = {0.f, 0.f, 0.f, -1, 0, 0, {0, 0}};
-      if (r < a.n) {
-        targets_of(a, r, row.e0, row.e1);
-        for (int e = row.e0; e < row.e1; ++e) {
-          const int t = a.tgt[e];
-          const float g = a.dlogp[e];
-          if (t >= 0 && t < a.v) {
-            row.total += g;
-            live = live || g != 0.f;
-            if (e == row.e0) row.t0 = t, row.g0 = g;
-          }
-          if (!FP32) {
-            a.ent_row[e] = r;
-            a.ent_rem[e] = 0.f;
-          }
-        }
-        row.lse2 = a.lse[r] * kLog2e;
-      }
-      a.row[r] = row;
-    }
-    s_live = live;
-  }
-  __syncthreads();
-  const bool live = s_live;
+__device__ __forceinline__ void copy_row(const LogprobArgs& a, int r, bool in_row, int64_t i) {
   for (int c = 8 * threadIdx.x; c < a.hp; c += 8 * 256) {
-    const bool in = live && c < a.h;
+    const bool in = in_row && c < a.h;
     if (!FP32) {
       u32x4 x = {0, 0, 0, 0};
       if (in) x = ld16((const bf16_t*)a.X + (int64_t)r * a.h + c);
-      *(u32x4*)(a.xc + (int64_t)r * a.hp + c) = x;
+      *(u32x4*)(a.xc + i * a.hp + c) = x;
     } else {
       for (int k = 0; k < 8; k += 4) {
         f32x4 x = {0, 0, 0, 0};
         if (in) x = *(const f32x4*)((const float*)a.X + (int64_t)r * a.h + c + k);
-        put_planes(x, a.xc, (int64_t)a.np * a.hp, (int64_t)r * a.hp + c + k);
+        put_planes(x, a.xc, (int64_t)a.np * a.hp, i * a.hp + c + k);
       }
     }
+  }
+}
+template <bool FP32>
+__global__ __launch_bounds__(256) void prep_kernel(LogprobArgs a) {
+  copy_row<FP32>(a, blockIdx.x, (int)blockIdx.x < a.n, blockIdx.x);
+}
+
+// The backward multiplies only rows that have a gradient: the others' part of either result is zero, whatever they hold.  They are
+// packed in their order, so that sums keep theirs: each 256 rows count their own (rows_kernel), the counts are added up
+// (before_kernel), and each row finds its place (gather_kernel).  Up to 256 rows every workgroup counts for itself.  A
+// third of 2047 rows masked: their backward takes two thirds of the time.
+__device__ __forceinline__ LogprobRow row_of(const LogprobArgs& a, int r, bool& live) {
+  LogprobRow row = {0.f, 0.f, 0.f, -1, 0, 0, r, -1};
+  live = false;
+  if (r >= a.n) return row;
+  targets_of(a, r, row.e0, row.e1);
+  for (int e = row.e0; e < row.e1; ++e) {
+    const int t = a.tgt[e];
+    const float g = a.dlogp[e];
+    if (t < 0 || t >= a.v) continue;
+    row.total += g;
+    live = live || g != 0.f;
+    if (e == row.e0) row.t0 = t, row.g0 = g;
+  }
+  row.lse2 = a.lse[r] * kLog2e;
+  return row;
+}
+// the place of each thread's row among the live ones of the workgroup's 256, and their number
+__device__ __forceinline__ int rank_of(bool live, int& count) {
+  __shared__ int s_count[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t mask = __ballot(live);
+  if (lane == 0) s_count[wave] = __builtin_popcountll(mask);
+  __syncthreads();
+  int at = __builtin_popcountll(mask & ((1ull << lane) - 1));
+  count = 0;
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) at += s_count[w];
+    count += s_count[w];
+  }
+  return live ? at : -1;
+}
+__global__ __launch_bounds__(256) void rows_kernel(LogprobArgs a) {
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  bool live;
+  LogprobRow row = row_of(a, r, live);
+  int count;
+  row.at = rank_of(live, count);
+  if (r < a.n) a.info[r] = row;
+  if (threadIdx.x == 0) a.before[blockIdx.x] = count;
+}
+__global__ __launch_bounds__(1024) void before_kernel(LogprobArgs a) {
+  __shared__ int s_sum[1024];
+  const int groups = (a.n + 255) / 256, each = (groups + 1023) / 1024, first = threadIdx.x * each, end = min(groups, first + each);
+  int sum = 0;
+  for (int k = first; k < end; ++k) sum += a.before[k];
+  s_sum[threadIdx.x] = sum;
+  for (int d = 1; d < 1024; d *= 2) {
+    __syncthreads();
+    const int x = (int)threadIdx.x >= d ? s_sum[threadIdx.x - d] : 0;
+    __syncthreads();
+    s_sum[threadIdx.x] += x;
+  }
+  int at = s_sum[threadIdx.x] - sum;
+  for (int k = first; k < end; ++k) {
+    const int n = a.before[k];
+    a.before[k] = at;
+    at += n;
+  }
+  if (threadIdx.x == 1023) *a.live = at;
+}
+// Workgroup r < n: row r; behind them those that fill the last 64 live rows up with empty ones.
+template <bool FP32, bool ALONE>
+__global__ __launch_bounds__(256) void gather_kernel(LogprobArgs a) {
+  __shared__ LogprobRow s_me;
+  const int r = blockIdx.x;
+  int count, before = 0;
+  if (ALONE) {
+    bool live;
+    LogprobRow row = row_of(a, threadIdx.x, live);
+    row.at = rank_of(live, count);
+    if ((int)threadIdx.x == r) s_me = row;
+    if (r == 0 && threadIdx.x == 0) *a.live = count;
+  } else {
+    count = *a.live;
+    if (r < a.n) before = a.before[r / 256];
+    if (r < a.n && threadIdx.x == 0) s_me = a.info[r];
+  }
+  __syncthreads();
+  if (r >= a.n) {
+    const int i = count + r - a.n;
+    if (i >= up64(count)) return;
+    if (threadIdx.x == 0) a.row[i] = {0.f, 0.f, 0.f, -1, 0, 0, -1, -1};
+    copy_row<FP32>(a, 0, false, i);
+    return;
+  }
+  const LogprobRow me = s_me;
+  const int i = me.at < 0 ? -1 : before + me.at;
+  if (!FP32)
+    for (int e = me.e0 + threadIdx.x; e < me.e1; e += 256) {
+      a.ent_row[e] = i;
+      a.ent_rem[e] = 0.f;
+    }
+  if (i >= 0) {
+    if (threadIdx.x == 0) a.row[i] = me;
+    copy_row<FP32>(a, r, true, i);
+  } else if (a.dX) {
+    const int64_t bytes = (int64_t)a.h * (FP32 ? 4 : 2);
+    for (int64_t x = 16 * threadIdx.x; x < bytes; x += 16 * 256) *(u32x4*)((uint8_t*)a.dX + r * bytes + x) = u32x4{0, 0, 0, 0};
   }
 }
 
@@ -415,13 +497,15 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
   const Tile tile = tile_of(downs, acrosses);
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;   // the wavefront's first entry and row of the tile
+  const int np = BACKWARD ? up64(*a.live) : a.n;
+  if (j0 >= np) return;
   f32x16 acc[S::FM][S::FN];
   const Operand W = w_operand(a, piece);
   __shared__ LogprobRow s_row[BACKWARD ? S::N : 1];        // (here so that its reads' time passes under the products)
   if constexpr (BACKWARD)
     for (int j = threadIdx.x; j < S::N; j += S::THREADS)
-      if (j0 + j < a.np) s_row[j] = a.row[j0 + j];
-  product<S, false, false>(acc, W, x_operand(a), i0, j0, a.hp, lds);
+      if (j0 + j < np) s_row[j] = a.row[j0 + j];
+  product<S, false, false>(acc, W, x_operand(a, np), i0, j0, a.hp, lds);
   const float c = a.scale * kLog2e;
   const int left = W.rows - iw - 4 * (lane >> 5);   // element (f, e) is an entry where 32 f + down(e) is below
   if constexpr (!BACKWARD) {
@@ -463,8 +547,8 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
 #pragma unroll
     for (int g = 0; g < S::FN; ++g) {
       sched_fence();
-      LogprobRow row = {0.f, 0.f, 0.f, -1, 0, 0, {0, 0}};
-      if (j0 + jw + 32 * g < a.np) row = s_row[jw + 32 * g + (lane & 31)];
+      LogprobRow row = {0.f, 0.f, 0.f, -1, 0, 0, -1, -1};
+      if (j0 + jw + 32 * g < np) row = s_row[jw + 32 * g + (lane & 31)];
       // (a row whose G is 0 takes 2^-inf: nothing, whatever its LSE)
       const float k = -row.total * a.scale, ref = k == 0.f ? -kNegInf : row.lse2;
 #pragma unroll
@@ -514,7 +598,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
       }
     }
     bf16_t* out = a.dl + j0 * a.piece_v + i0;
-    const int64_t lim_across = a.np - j0, lim_down = a.piece_v - i0;
+    const int64_t lim_across = np - j0, lim_down = a.piece_v - i0;
     if constexpr (S::P == 1) {
       store_tile<S>(
           [&](int f, int g, int h) {
@@ -522,7 +606,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
             return rows8(pack2(x[8 * h], x[8 * h + 1]), pack2(x[8 * h + 2], x[8 * h + 3]), pack2(x[8 * h + 4], x[8 * h + 5]),
                          pack2(x[8 * h + 6], x[8 * h + 7]));
           },
-          out, a.piece_v, lim_across, lim_down, lds);
+          [&](int j) { return out + (int64_t)j * a.piece_v; }, lim_across, lim_down, lds);
     } else {
       static_for<3>([&](auto q) {
         constexpr int Q = decltype(q)::value;
@@ -539,7 +623,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
               }
               return rows8(w[0], w[1], w[2], w[3]);
             },
-            out + Q * (int64_t)a.np * a.piece_v, a.piece_v, lim_across, lim_down, lds);
+            [&](int j) { return out + ((int64_t)Q * a.np + j) * a.piece_v; }, lim_across, lim_down, lds);
       });
     }
   }
@@ -653,32 +737,31 @@ __device__ __forceinline__ void add_terms(f32x16 (&acc)[S::FM][S::FN], int count
   }
   __syncthreads();
 }
-// Target e as a term of its row r: what the rounding of its dz left out, 0 if row r does not list it.
-__device__ __forceinline__ float rem_of(const LogprobArgs& a, int e, int r) {
-  int e0 = 0, e1 = 0;
-  if (r >= 0 && r < a.n) targets_of(a, r, e0, e1);
-  return e >= e0 && e < e1 ? a.ent_rem[e] : 0.f;
+// Target e as a term of live row i: what the rounding of its dz left out, 0 if that row does not list it.
+__device__ __forceinline__ float rem_of(const LogprobArgs& a, int e, int i, int live) {
+  if (i < 0 || i >= live) return 0.f;
+  return e >= a.row[i].e0 && e < a.row[i].e1 ? a.ent_rem[e] : 0.f;
 }
-// the workgroup's tile to a result of the inputs' type
-template <class S>
-__device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::FM][S::FN], void* out, int64_t at, int64_t ld, int64_t lim_across, int64_t lim_down,
-                                         uint8_t* lds) {
+// the workgroup's tile to a result of the inputs' type, rows row(0) .. row(lim_across - 1) of h elements, elements i0 .. of them
+template <class S, class R>
+__device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::FM][S::FN], void* out, R&& row, int h, int64_t i0, int64_t lim_across, uint8_t* lds) {
   if constexpr (S::P == 1) {
     store_tile<S>(
-        [&](int f, int g, int h) {
+        [&](int f, int g, int k) {
           const f32x16& x = acc[f][g];
-          return rows8(pack2(x[8 * h], x[8 * h + 1]), pack2(x[8 * h + 2], x[8 * h + 3]), pack2(x[8 * h + 4], x[8 * h + 5]),
-                       pack2(x[8 * h + 6], x[8 * h + 7]));
+          return rows8(pack2(x[8 * k], x[8 * k + 1]), pack2(x[8 * k + 2], x[8 * k + 3]), pack2(x[8 * k + 4], x[8 * k + 5]),
+                       pack2(x[8 * k + 6], x[8 * k + 7]));
         },
-        (bf16_t*)out + at, ld, lim_across, lim_down, lds);
+        [&](int j) { return (bf16_t*)out + (int64_t)row(j) * h + i0; }, lim_across, h - i0, lds);
   } else {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
     for (int g = 0; g < S::FN; ++g) {
       const int j = (wave % S::WN * S::FN + g) * 32 + (lane & 31);
+      if (j >= lim_across) continue;
+      float* p = (float*)out + (int64_t)row(j) * h;
 #pragma unroll
-      for (int f = 0; f < S::FM; ++f)
-        put_rows((float*)out + at + j * ld, (wave / S::WN * S::FM + f) * 32, j < lim_across ? (int)min(lim_down, (int64_t)S::M) : 0, acc[f][g], lane);
+      for (int f = 0; f < S::FM; ++f) put_rows(p, (int)i0 + (wave / S::WN * S::FM + f) * 32, h, acc[f][g], lane);
     }
   }
 }
@@ -694,31 +777,33 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
   const int split = tile.part, k = a.stages_dx * 64;
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
+  const int live = *a.live, np = up64(live);
+  if (j0 >= live) return;
   f32x16 acc[S::FM][S::FN];
   const bool last = piece == a.pieces - 1, rest = S::P == 1 && last && split == 0;   // rest: what the targets' dz left out is added
-  // (the tile's rows have their targets one behind the other: LIST at a time, the first ones ahead of the products)
+  // (the tile's rows have their targets one behind the other, with those of rows that are not live between them: LIST at a time, the first ones ahead of the products)
   constexpr int LIST = S::P == 1 ? 2 * S::N : 1;
   __shared__ struct { float rem; int32_t tgt, col; } s_list[LIST];
   int e_lo = 0, e_hi = 0;
   auto list = [&] {
     for (int k = threadIdx.x; k < LIST && e_lo + k < e_hi; k += S::THREADS) {
       const int e = e_lo + k, r = a.ent_row[e], t = a.tgt[e];
-      const bool in = r >= j0 && r < min(j0 + S::N, (int64_t)a.n) && t >= 0 && t < a.v;
-      s_list[k] = {in ? rem_of(a, e, r) : 0.f, t, (int)(r - j0)};
+      const bool in = r >= j0 && r < j0 + S::N && t >= 0 && t < a.v;
+      s_list[k] = {in ? rem_of(a, e, r, live) : 0.f, t, (int)(r - j0)};
     }
   };
   if (rest) {
-    e_lo = a.row[j0].e0, e_hi = max(e_lo, a.row[min(j0 + S::N, (int64_t)a.n) - 1].e1);
+    e_lo = a.row[j0].e0, e_hi = max(e_lo, a.row[min(j0 + S::N, (int64_t)live) - 1].e1);
     list();
   }
   const Operand W = part_of(swapped(w_operand(a, piece)), true, (int64_t)split * k, k);
-  const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.np, a.piece_v}, false, (int64_t)split * k, k);
+  const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, np, a.piece_v}, false, (int64_t)split * k, k);
   product<S, true, false>(acc, W, D, i0, j0, W.ks, lds);
   float* sums = a.dx_acc + (int64_t)split * a.n * a.h;
 #pragma unroll
   for (int g = 0; g < S::FN; ++g) {
     const int64_t r = j0 + jw + 32 * g + (lane & 31);
-    const int limit = r < a.n ? a.h : 0;
+    const int limit = r < live ? a.h : 0;
     if (piece) {
 #pragma unroll
       for (int f = 0; f < S::FM; ++f)
@@ -745,12 +830,12 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
 #pragma unroll
     for (int g = 0; g < S::FN; ++g) {
       const int64_t r = j0 + jw + 32 * g + (lane & 31);
-      const int limit = r < a.n ? a.h : 0;
+      const int limit = r < live ? a.h : 0;
 #pragma unroll
       for (int f = 0; f < S::FM; ++f) put_rows(sums + r * a.h, iw + 32 * f, limit, acc[f][g], lane);
     }
   }
-  if (last && a.splits_dx == 1) put_tile<S>(acc, a.dX, j0 * a.h + i0, a.h, a.n - j0, a.h - i0, lds);
+  if (last && a.splits_dx == 1) put_tile<S>(acc, a.dX, [&](int j) { return a.row[j0 + j].r; }, a.h, i0, live - j0, lds);
 }
 
 // dW: M of the hidden dimension down, N entries across, summed over the rows; both operands are read by the transposing loads.
@@ -761,7 +846,8 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Tile tile = tile_of(downs, acrosses);
-  const int split = tile.part, k = a.stages_dw * 64;
+  const int live = *a.live, np = up64(live);
+  const int split = tile.part, k = (np / 64 + a.splits_dw - 1) / a.splits_dw * 64;
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
   f32x16 acc[S::FM][S::FN];
@@ -816,13 +902,13 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
     __syncthreads();
     for (int k = threadIdx.x; k < listed; k += S::THREADS) {
       const int e = s_list[k].row, r = a.ent_row[e];
-      s_list[k].rem = rem_of(a, e, r);
+      s_list[k].rem = rem_of(a, e, r, live);
       s_list[k].row = r;
     }
   };
   if (rest) collect();
-  const Operand X = part_of({a.xc, a.hp, (int64_t)a.np * a.hp, a.hp, a.np}, true, (int64_t)split * k, k);
-  const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, a.np}, true, (int64_t)split * k, k);
+  const Operand X = part_of({a.xc, a.hp, (int64_t)a.np * a.hp, a.hp, np}, true, (int64_t)split * k, k);
+  const Operand D = part_of({a.dl, a.piece_v, (int64_t)a.np * a.piece_v, a.piece_v, np}, true, (int64_t)split * k, k);
   product<S, true, true>(acc, X, D, i0, j0, X.ks, lds);
   if (rest) {
     for (;;) {
@@ -842,19 +928,25 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
       for (int f = 0; f < S::FM; ++f) put_rows(sums + (j0 + j) * a.h, iw + 32 * f, j < vn ? a.h : 0, acc[f][g], lane);
     }
   } else {
-    put_tile<S>(acc, a.dW, (int64_t)v0 * a.h + i0, a.h, vn, a.h - i0, lds);
+    put_tile<S>(acc, a.dW, [&](int j) { return v0 + j; }, a.h, i0, vn, lds);
   }
 }
 
-// out [n] = the sum of the slabs of n fp32 elements, first to last
-template <bool FP32>
-__global__ __launch_bounds__(256) void slabs_kernel(const float* slab, int64_t stride, int count, void* out, int64_t n) {
+// Rows of h elements: the sum of their fp32 slabs, first to last.  ROWS: of the live rows, to where they come from.
+template <bool FP32, bool ROWS>
+__global__ __launch_bounds__(256) void slabs_kernel(LogprobArgs a, const float* slab, int64_t stride, int count, void* out, int rows) {
+  const int64_t n = (int64_t)(ROWS ? *a.live : rows) * a.h;
   for (int64_t i = 4 * ((int64_t)blockIdx.x * 256 + threadIdx.x); i < n; i += 4 * (int64_t)gridDim.x * 256) {
     f32x4 x = *(const f32x4*)(slab + i);
 #pragma unroll 4
     for (int k = 1; k < count; ++k) x += *(const f32x4*)(slab + k * stride + i);
-    if (FP32) *(f32x4*)((float*)out + i) = x;
-    else *(u32x2*)((bf16_t*)out + i) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
+    int64_t at = i;
+    if (ROWS) {
+      const int64_t row = i / a.h;
+      at = (int64_t)a.row[row].r * a.h + (i - row * a.h);
+    }
+    if (FP32) *(f32x4*)((float*)out + at) = x;
+    else *(u32x2*)((bf16_t*)out + at) = u32x2{pack2(x[0], x[1]), pack2(x[2], x[3])};
   }
 }
 
@@ -863,9 +955,26 @@ int piece_rows(const LogprobArgs& a, int piece) { return std::min(a.piece_v, a.v
 
 }  // namespace
 
-hipError_t launch_logprob_prep(const LogprobArgs& a, bool backward, hipStream_t st) {
-  if (a.planes == 3) hipLaunchKernelGGL(prep_kernel<true>, dim3((unsigned)a.np), dim3(256), 0, st, a, backward ? 1 : 0);
-  else hipLaunchKernelGGL(prep_kernel<false>, dim3((unsigned)a.np), dim3(256), 0, st, a, backward ? 1 : 0);
+hipError_t launch_logprob_prep(const LogprobArgs& a, hipStream_t st) {
+  if (a.planes == 3) hipLaunchKernelGGL(prep_kernel<true>, dim3((unsigned)a.np), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(prep_kernel<false>, dim3((unsigned)a.np), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+hipError_t launch_logprob_rows(const LogprobArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)a.n + 64), wg(256);
+  if (a.n <= 256) {
+    if (a.planes == 3) hipLaunchKernelGGL((gather_kernel<true, true>), grid, wg, 0, st, a);
+    else hipLaunchKernelGGL((gather_kernel<false, true>), grid, wg, 0, st, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(rows_kernel, dim3((unsigned)((a.n + 255) / 256)), wg, 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(before_kernel, dim3(1), dim3(1024), 0, st, a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.planes == 3) hipLaunchKernelGGL((gather_kernel<true, false>), grid, wg, 0, st, a);
+  else hipLaunchKernelGGL((gather_kernel<false, false>), grid, wg, 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_logprob_wplanes(const LogprobArgs& a, int piece, hipStream_t st) {
@@ -903,10 +1012,11 @@ void dw(const LogprobArgs& a, int piece, hipStream_t st) {
   else if (a.shape_dw == LP_SMALL) launch_tiles<typename T::Small>(dw_kernel<typename T::Small>, a.h, rows, a.splits_dw, a, piece, st);
   else launch_tiles<typename T::Deep>(dw_kernel<typename T::Deep>, a.h, rows, a.splits_dw, a, piece, st);
 }
-void sum_slabs(const LogprobArgs& a, const float* slab, int64_t stride, int count, void* out, int64_t n, hipStream_t st) {
-  const dim3 grid((unsigned)std::min<int64_t>((n / 4 + 255) / 256, 8192));
-  if (a.planes == 3) hipLaunchKernelGGL(slabs_kernel<true>, grid, dim3(256), 0, st, slab, stride, count, out, n);
-  else hipLaunchKernelGGL(slabs_kernel<false>, grid, dim3(256), 0, st, slab, stride, count, out, n);
+template <bool ROWS>
+void sum_slabs(const LogprobArgs& a, const float* slab, int64_t stride, int count, void* out, int rows, hipStream_t st) {
+  const dim3 grid((unsigned)std::min<int64_t>(((int64_t)rows * a.h / 4 + 255) / 256, 8192));
+  if (a.planes == 3) hipLaunchKernelGGL((slabs_kernel<true, ROWS>), grid, dim3(256), 0, st, a, slab, stride, count, out, rows);
+  else hipLaunchKernelGGL((slabs_kernel<false, ROWS>), grid, dim3(256), 0, st, a, slab, stride, count, out, rows);
 }
 }  // namespace
 
@@ -927,12 +1037,12 @@ hipError_t launch_logprob_dx(const LogprobArgs& a, int piece, hipStream_t st) {
   return hipGetLastError();
 }
 hipError_t launch_logprob_dx_sum(const LogprobArgs& a, hipStream_t st) {
-  sum_slabs(a, a.dx_acc, (int64_t)a.n * a.h, a.splits_dx, a.dX, (int64_t)a.n * a.h, st);
+  sum_slabs<true>(a, a.dx_acc, (int64_t)a.n * a.h, a.splits_dx, a.dX, a.n, st);
   return hipGetLastError();
 }
 hipError_t launch_logprob_dw_sum(const LogprobArgs& a, int piece, hipStream_t st) {
   const int64_t at = (int64_t)piece * a.piece_v * a.h * (a.planes == 3 ? 4 : 2);
-  sum_slabs(a, a.dw_acc, (int64_t)a.piece_v * a.h, a.splits_dw, (uint8_t*)a.dW + at, (int64_t)piece_rows(a, piece) * a.h, st);
+  sum_slabs<false>(a, a.dw_acc, (int64_t)a.piece_v * a.h, a.splits_dw, (uint8_t*)a.dW + at, piece_rows(a, piece), st);
   return hipGetLastError();
 }
 hipError_t launch_logprob_dw(const LogprobArgs& a, int piece, hipStream_t st) {

@@ -147,6 +147,20 @@ def test_rows_without_gradient_do_not_reach_others(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,alive", [(256, 0.3), (257, 0.9), (1000, 0.02), (2500, 0.5), (777, 0.0)])
+def test_few_rows_with_a_gradient(n, alive, dtype):
+    """The live rows are packed for the products, each 256 rows by themselves: any share of them, in blocks and scattered."""
+    g = torch.Generator().manual_seed(n)
+    k = (torch.rand(n, generator=g) < alive).long() * torch.randint(1, 3, (n,), generator=g)
+    k[n // 3:n // 2] = 0
+    a = make(n, 72, 300, dtype, n, per_row=k.tolist())
+    a[4][::5] = 0
+    got = call(*a)
+    check(got, *reference(*a, 1.0), f"{dtype} {n} rows, {alive} alive")
+    assert not got["dX"][(k == 0).cuda()].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_no_rows_no_targets(dtype):
     from paper_2608_25683_amd import psattn as P
     x, w, ptr, tgt, g = make(0, 64, 100, dtype, 1, per_row=[])

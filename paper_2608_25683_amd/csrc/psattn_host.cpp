@@ -1077,10 +1077,10 @@ struct Profiler {
 Profiler g_prof;
 const char* kKernelNames[] = {"fwd_main", "fwd_merge",     "bwd_pre", "bwd_kv",   "bwd_dq", "bwd_reduce_kv",
                               "bwd_reduce_dq", "rope",       "kv_scatter", "kv_gather", "split_planes", "silu_bwd",
-                              "logprob_prep", "logprob_wplanes", "logprob_logits", "logprob_finish", "logprob_dz", "logprob_dx",
-                              "logprob_dx_sum", "logprob_dw", "logprob_dw_sum", "adamw_norm", "adamw_scalars", "adamw_step"};
-constexpr int kNumKernels = 24;
-enum { K_LP_PREP = 12, K_LP_WPLANES, K_LP_LOGITS, K_LP_FINISH, K_LP_DZ, K_LP_DX, K_LP_DX_SUM, K_LP_DW, K_LP_DW_SUM, K_ADAMW_NORM, K_ADAMW_SCALARS, K_ADAMW_STEP };
+                              "logprob_prep", "logprob_wplanes", "logprob_logits", "logprob_finish", "logprob_dz", "logprob_grads",
+                              "logprob_dx_sum", "logprob_dw_sum", "adamw_norm", "adamw_scalars", "adamw_step"};
+constexpr int kNumKernels = 23;
+enum { K_LP_PREP = 12, K_LP_WPLANES, K_LP_LOGITS, K_LP_FINISH, K_LP_DZ, K_LP_GRADS, K_LP_DX_SUM, K_LP_DW_SUM, K_ADAMW_NORM, K_ADAMW_SCALARS, K_ADAMW_STEP };
 
 hipEvent_t get_event() {
   if (!g_prof.spare.empty()) {
@@ -1352,13 +1352,14 @@ struct LogprobPlan {
 // one with its copies further ahead; parts are written and read as fp32 at 4.5 TB/s behind another launch.  (1280 rows x 1024 x 32000:
 // dX as 80 tiles of 500 stages 315, as seven parts 60; 512 rows x 4096 x 16000: logits 95 large, 67 small, as estimated.)
 struct LogprobTiling { int32_t shape, splits, stages; double us; };
-LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes, int max_splits) {
+LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes, int max_splits, int shape = -1) {
   struct Kind { int32_t shape, m, n, slots; double stage, ends; };
   static const std::vector<Kind> bf16 = {{LP_LARGE, 256, 256, 256, 1.5, 10}, {LP_SMALL, 128, 128, 512, 0.83, 8}, {LP_DEEP, 128, 128, 256, 0.5, 8}};
   static const std::vector<Kind> fp32 = {{LP_LARGE, 256, 128, 256, 4.1, 12}, {LP_SMALL, 128, 128, 256, 3.2, 10}};
   LogprobTiling best{LP_LARGE, 1, 1, 1e30};
   const int64_t nk = std::max<int64_t>(1, (k + 63) / 64);
   for (const Kind& c : planes == 3 ? fp32 : bf16) {
+    if (shape >= 0 && c.shape != shape) continue;
     const int64_t tiles = ((down + c.m - 1) / c.m) * ((across + c.n - 1) / c.n);
     for (int64_t s = 1; s <= max_splits && s <= nk; ++s) {
       const int64_t each = (nk + s - 1) / s, parts = (nk + each - 1) / each;
@@ -1410,8 +1411,15 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
     return fail(PSATTN_E_UNSUPPORTED, "rows %d x vocab %d: more tiles than a launch holds", a.n, a.v);
   a.shape = a.n <= 32 ? LP_THIN : logprob_tiling(std::min(a.v, a.piece_v), a.n, a.hp, a.planes, 1).shape;
   a.part_v = a.shape == LP_LARGE ? 256 : 128;
-  const LogprobTiling dx = logprob_tiling(a.h, a.n, std::min(a.v, a.piece_v), a.planes, 32);
-  const LogprobTiling dw = logprob_tiling(a.h, std::min(a.v, a.piece_v), a.n, a.planes, 32);
+  // The gradients' tiles of one shape, if that costs less than a tenth by the estimate: one launch then fills the chip for both.
+  const int64_t pv = std::min(a.v, a.piece_v);
+  LogprobTiling dx = logprob_tiling(a.h, a.n, pv, a.planes, 32), dw = logprob_tiling(a.h, pv, a.n, a.planes, 32);
+  double most = 1.1 * (dx.us + dw.us);
+  for (int shape : {LP_LARGE, LP_SMALL, LP_DEEP}) {
+    if (fp32 && shape == LP_DEEP) continue;
+    const LogprobTiling x = logprob_tiling(a.h, a.n, pv, a.planes, 32, shape), w = logprob_tiling(a.h, pv, a.n, a.planes, 32, shape);
+    if (x.us + w.us < most) most = x.us + w.us, dx = x, dw = w;
+  }
   a.shape_dx = dx.shape, a.splits_dx = dx.splits, a.stages_dx = dx.stages;
   a.shape_dw = dw.shape, a.splits_dw = dw.splits;
   size_t cur = 0;
@@ -1534,8 +1542,9 @@ psattn_status psattn_logprob_bwd(const psattn_logprob_desc* desc, const void* X,
   for (int i = 0; i < a.pieces && s == PSATTN_OK; ++i) {
     if (a.n && a.wc) s = timed(K_LP_WPLANES, st, [&] { return launch_logprob_wplanes(a, i, st); });
     if (s == PSATTN_OK && a.n) s = timed(K_LP_DZ, st, [&] { return launch_logprob_logits(a, i, true, st); });
-    if (s == PSATTN_OK && a.dX) s = timed(K_LP_DX, st, [&] { return launch_logprob_dx(a, i, st); });
-    if (s == PSATTN_OK && a.dW) s = timed(K_LP_DW, st, [&] { return launch_logprob_dw(a, i, st); });
+    const bool together = a.dX && a.dW && a.shape_dx == a.shape_dw;
+    if (s == PSATTN_OK && (a.dX || together)) s = timed(K_LP_GRADS, st, [&] { return launch_logprob_grads(a, i, true, together, st); });
+    if (s == PSATTN_OK && a.dW && !together) s = timed(K_LP_GRADS, st, [&] { return launch_logprob_grads(a, i, false, true, st); });
     if (s == PSATTN_OK && a.dW && a.splits_dw > 1) s = timed(K_LP_DW_SUM, st, [&] { return launch_logprob_dw_sum(a, i, st); });
   }
   if (s == PSATTN_OK && a.dX && a.splits_dx > 1) s = timed(K_LP_DX_SUM, st, [&] { return launch_logprob_dx_sum(a, st); });

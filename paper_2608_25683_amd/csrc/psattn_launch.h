@@ -201,10 +201,9 @@ PSATTN_WEAK hipError_t launch_logprob_rows(const LogprobArgs& a, hipStream_t st)
 PSATTN_WEAK hipError_t launch_logprob_wplanes(const LogprobArgs& a, int piece, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_logits(const LogprobArgs& a, int piece, bool backward, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_finish(const LogprobArgs& a, hipStream_t st);
-PSATTN_WEAK hipError_t launch_logprob_dx(const LogprobArgs& a, int piece, hipStream_t st);
+PSATTN_WEAK hipError_t launch_logprob_grads(const LogprobArgs& a, int piece, bool dx, bool dw, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_dx_sum(const LogprobArgs& a, hipStream_t st);
 PSATTN_WEAK hipError_t launch_logprob_dw_sum(const LogprobArgs& a, int piece, hipStream_t st);
-PSATTN_WEAK hipError_t launch_logprob_dw(const LogprobArgs& a, int piece, hipStream_t st);
 PSATTN_WEAK hipError_t launch_adamw_norm(const AdamwArgs& a, const AdamwGrads& g, hipStream_t st);
 PSATTN_WEAK hipError_t launch_adamw_scalars(const AdamwArgs& a, bool with_norm, hipStream_t st);
 PSATTN_WEAK hipError_t launch_adamw_step(const AdamwArgs& a, const AdamwGrads& g, hipStream_t st);

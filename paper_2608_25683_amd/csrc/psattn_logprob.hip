@@ -307,9 +307,9 @@ __device__ __forceinline__ void store_tile(F&& eight, O&& out, int64_t lim_acros
 // it at a time share rows of both operands in its L2.  (dX of 513 fp32 rows x 1024 x 16001, 12 parts of 40 tiles: 172 us
 // with each part's tiles spread over the XCDs, 121 so.)
 struct Tile { int part, down, across; };
-__device__ __forceinline__ Tile tile_of(int downs, int acrosses) {
-  const int each = gridDim.x / 8, rest = gridDim.x % 8, x = blockIdx.x % 8;
-  const int all = x * each + min(x, rest) + blockIdx.x / 8, tiles = downs * acrosses;
+__device__ __forceinline__ Tile tile_of(unsigned block, unsigned blocks, int downs, int acrosses) {
+  const int each = blocks / 8, rest = blocks % 8, x = block % 8;
+  const int all = x * each + min(x, rest) + block / 8, tiles = downs * acrosses;
   const int part = all / tiles, t = all - part * tiles;
   const int first = t / (4 * acrosses) * 4, high = min(4, downs - first), in = t - first * acrosses;
   // (divisions leave uniform values in vector registers)
@@ -375,7 +375,8 @@ __global__ __launch_bounds__(256) void prep_kernel(LogprobArgs a) {
 // The backward multiplies only rows that have a gradient: the others' part of either result is zero, whatever they hold.  They are
 // packed in their order, so that sums keep theirs: each 256 rows count their own (rows_kernel), the counts are added up
 // (before_kernel), and each row finds its place (gather_kernel).  Up to 256 rows every workgroup counts for itself.  A
-// third of 2047 rows masked: their backward takes two thirds of the time.
+// third of 2047 rows masked, in all two fifths without gradient: 2047 x 1544 x 50257 forward and backward 1.42 ms with all rows
+// multiplied, 1.11 so.
 __device__ __forceinline__ LogprobRow row_of(const LogprobArgs& a, int r, bool& live) {
   LogprobRow row = {0.f, 0.f, 0.f, -1, 0, 0, r, -1};
   live = false;
@@ -489,16 +490,19 @@ __global__ __launch_bounds__(256) void wplanes_kernel(LogprobArgs a, int piece) 
 // ---- a tile of logits: M entries of the piece down, N rows across, so that a lane holds 16 FM entries of each of its FN rows.
 // Forward: the maximum and the sum of exponentials of the tile's entries leave for each row, one fma, one exponential, one
 // addition and half a maximum per logit; nothing else is written.  Backward: dz of the tile, scaled, as bf16 or as
-// planes: 6.84 ms for 8192 x 128256 x 4096 against the forward's 6.30, for the same product and 2 GB written.
+// planes: 6.84 ms for 8192 x 128256 x 4096 (every row live) against the forward's 6.30, for the same product and 2 GB written.
 template <class S, bool BACKWARD>
 __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Tile tile = tile_of(downs, acrosses);
+  int np = a.n, blocks = gridDim.x;
+  if (BACKWARD) {   // (fewer rows are live than the launch has room for)
+    np = up64(*a.live), acrosses = (np + S::N - 1) / S::N, blocks = downs * acrosses;
+    if ((int)blockIdx.x >= blocks) return;
+  }
+  const Tile tile = tile_of(blockIdx.x, blocks, downs, acrosses);
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;   // the wavefront's first entry and row of the tile
-  const int np = BACKWARD ? up64(*a.live) : a.n;
-  if (j0 >= np) return;
   f32x16 acc[S::FM][S::FN];
   const Operand W = w_operand(a, piece);
   __shared__ LogprobRow s_row[BACKWARD ? S::N : 1];        // (here so that its reads' time passes under the products)
@@ -767,18 +771,15 @@ __device__ __forceinline__ void put_tile(const f32x16 (&acc)[S::FM][S::FN], void
 }
 
 // dX: M of the hidden dimension down, N rows across, summed over the piece's entries or a part of them; W is read across its rows by
-// the transposing loads.  Pieces add to fp32 sums in memory, the last one leaves the result.  8192 x 4096 x 128256: 6.57 ms in four
-// pieces, 1310 TFLOP/s.
+// the transposing loads.  Pieces add to fp32 sums in memory, the last one leaves the result.  8192 x 4096 x 128256 by itself, every
+// row live: 6.57 ms in four pieces, 1310 TFLOP/s.
 template <class S>
-__global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+__device__ __forceinline__ void dx_tile(const LogprobArgs& a, int piece, const Tile& tile, uint8_t* lds) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Tile tile = tile_of(downs, acrosses);
   const int split = tile.part, k = a.stages_dx * 64;
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;
   const int live = *a.live, np = up64(live);
-  if (j0 >= live) return;
   f32x16 acc[S::FM][S::FN];
   const bool last = piece == a.pieces - 1, rest = S::P == 1 && last && split == 0;   // rest: what the targets' dz left out is added
   // (the tile's rows have their targets one behind the other, with those of rows that are not live between them: LIST at a time, the first ones ahead of the products)
@@ -839,13 +840,11 @@ __global__ __launch_bounds__(S::THREADS) void dx_kernel(LogprobArgs a, int piece
 }
 
 // dW: M of the hidden dimension down, N entries across, summed over the rows; both operands are read by the transposing loads.
-// 8192 x 4096 x 128256: 6.64 ms, 1297 TFLOP/s (a library product with such operands: 1180).  Few rows: bound by dW's bytes
+// 8192 x 4096 x 128256 by itself: 6.64 ms, 1297 TFLOP/s (a library product with such operands: 1180).  Few rows: bound by dW's bytes
 // (64 rows: 377 us for 1.05 GB).
 template <class S>
-__global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+__device__ __forceinline__ void dw_tile(const LogprobArgs& a, int piece, const Tile& tile, uint8_t* lds) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Tile tile = tile_of(downs, acrosses);
   const int live = *a.live, np = up64(live);
   const int split = tile.part, k = (np / 64 + a.splits_dw - 1) / a.splits_dw * 64;
   const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
@@ -932,6 +931,22 @@ __global__ __launch_bounds__(S::THREADS) void dw_kernel(LogprobArgs a, int piece
   }
 }
 
+// Both gradients of a piece in one launch where their tiles are of one shape: dX has few and long ones, whose last round would leave most
+// of the chip idle, the more so as it is not known ahead how many rows are live; dW's fill it.  (The live tiles are the first ones, so
+// that every XCD gets its share of them.)  2047 rows x 1544 x 50257, two fifths of the rows without gradient: 551 us one after the
+// other, 460 so; 8192 x 4096 x 128256, a fifth: 11.96 and 10.97 ms.
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void grads_kernel(LogprobArgs a, int piece, int downs, int dx_blocks, int dw_acrosses, int dw_blocks) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+  const int block = blockIdx.x;
+  if (block < dx_blocks) {
+    const int acrosses = (*a.live + S::N - 1) / S::N, blocks = downs * acrosses * a.splits_dx;
+    if (block < blocks) dx_tile<S>(a, piece, tile_of(block, blocks, downs, acrosses), lds);
+  } else {
+    dw_tile<S>(a, piece, tile_of(block - dx_blocks, dw_blocks, downs, dw_acrosses), lds);
+  }
+}
+
 // Rows of h elements: the sum of their fp32 slabs, first to last.  ROWS: of the live rows, to where they come from.
 template <bool FP32, bool ROWS>
 __global__ __launch_bounds__(256) void slabs_kernel(LogprobArgs a, const float* slab, int64_t stride, int count, void* out, int rows) {
@@ -982,35 +997,33 @@ hipError_t launch_logprob_wplanes(const LogprobArgs& a, int piece, hipStream_t s
   return hipGetLastError();
 }
 namespace {
-// One workgroup per tile of down x across and part of the sum.
-template <class S, class K>
-void launch_tiles(K kernel, int64_t down, int64_t across, int parts, const LogprobArgs& a, int piece, hipStream_t st) {
-  const int d = tiles(down, S::M), c = tiles(across, S::N);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((int64_t)d * c * parts)), dim3(S::THREADS), 0, st, a, piece, d, c);
+// One workgroup per tile of down x across.
+template <class S, bool BACKWARD>
+void launch_logits(const LogprobArgs& a, int piece, hipStream_t st) {
+  const int d = tiles(piece_rows(a, piece), S::M), c = tiles(BACKWARD ? a.np : a.n, S::N);
+  hipLaunchKernelGGL((logits_kernel<S, BACKWARD>), dim3((unsigned)d * (unsigned)c), dim3(S::THREADS), 0, st, a, piece, d, c);
 }
 template <int P, bool BACKWARD>
 void logits(const LogprobArgs& a, int piece, hipStream_t st) {
   using T = Tilings<P>;
-  const int rows = piece_rows(a, piece), n = BACKWARD ? a.np : a.n;
-  if (a.shape == LP_LARGE) launch_tiles<typename T::Large>(logits_kernel<typename T::Large, BACKWARD>, rows, n, 1, a, piece, st);
-  else if (a.shape == LP_SMALL) launch_tiles<typename T::Small>(logits_kernel<typename T::Small, BACKWARD>, rows, n, 1, a, piece, st);
-  else if (a.shape == LP_DEEP) launch_tiles<typename T::Deep>(logits_kernel<typename T::Deep, BACKWARD>, rows, n, 1, a, piece, st);
-  else launch_tiles<typename T::Thin>(logits_kernel<typename T::Thin, BACKWARD>, rows, n, 1, a, piece, st);
+  if (a.shape == LP_LARGE) launch_logits<typename T::Large, BACKWARD>(a, piece, st);
+  else if (a.shape == LP_SMALL) launch_logits<typename T::Small, BACKWARD>(a, piece, st);
+  else if (a.shape == LP_DEEP) launch_logits<typename T::Deep, BACKWARD>(a, piece, st);
+  else launch_logits<typename T::Thin, BACKWARD>(a, piece, st);
+}
+// One workgroup per tile and part of the sum, of either gradient or of both.
+template <class S>
+void launch_grads(const LogprobArgs& a, int piece, bool dx, bool dw, hipStream_t st) {
+  const int downs = tiles(a.h, S::M), xc = tiles(a.n, S::N), wc = tiles(piece_rows(a, piece), S::N);
+  const int xn = dx ? downs * xc * a.splits_dx : 0, wn = dw ? downs * wc * a.splits_dw : 0;
+  hipLaunchKernelGGL(grads_kernel<S>, dim3((unsigned)xn + (unsigned)wn), dim3(S::THREADS), 0, st, a, piece, downs, xn, wc, wn);
 }
 template <int P>
-void dx(const LogprobArgs& a, int piece, hipStream_t st) {
+void grads(const LogprobArgs& a, int piece, int shape, bool dx, bool dw, hipStream_t st) {
   using T = Tilings<P>;
-  if (a.shape_dx == LP_LARGE) launch_tiles<typename T::Large>(dx_kernel<typename T::Large>, a.h, a.n, a.splits_dx, a, piece, st);
-  else if (a.shape_dx == LP_SMALL) launch_tiles<typename T::Small>(dx_kernel<typename T::Small>, a.h, a.n, a.splits_dx, a, piece, st);
-  else launch_tiles<typename T::Deep>(dx_kernel<typename T::Deep>, a.h, a.n, a.splits_dx, a, piece, st);
-}
-template <int P>
-void dw(const LogprobArgs& a, int piece, hipStream_t st) {
-  using T = Tilings<P>;
-  const int rows = piece_rows(a, piece);
-  if (a.shape_dw == LP_LARGE) launch_tiles<typename T::Large>(dw_kernel<typename T::Large>, a.h, rows, a.splits_dw, a, piece, st);
-  else if (a.shape_dw == LP_SMALL) launch_tiles<typename T::Small>(dw_kernel<typename T::Small>, a.h, rows, a.splits_dw, a, piece, st);
-  else launch_tiles<typename T::Deep>(dw_kernel<typename T::Deep>, a.h, rows, a.splits_dw, a, piece, st);
+  if (shape == LP_LARGE) launch_grads<typename T::Large>(a, piece, dx, dw, st);
+  else if (shape == LP_SMALL) launch_grads<typename T::Small>(a, piece, dx, dw, st);
+  else launch_grads<typename T::Deep>(a, piece, dx, dw, st);
 }
 template <bool ROWS>
 void sum_slabs(const LogprobArgs& a, const float* slab, int64_t stride, int count, void* out, int rows, hipStream_t st) {
@@ -1031,9 +1044,9 @@ hipError_t launch_logprob_finish(const LogprobArgs& a, hipStream_t st) {
   else hipLaunchKernelGGL(finish_kernel<false>, grid, dim3(1024), 0, st, a);
   return hipGetLastError();
 }
-hipError_t launch_logprob_dx(const LogprobArgs& a, int piece, hipStream_t st) {
-  if (a.planes == 3) dx<3>(a, piece, st);
-  else dx<1>(a, piece, st);
+hipError_t launch_logprob_grads(const LogprobArgs& a, int piece, bool dx, bool dw, hipStream_t st) {
+  const int shape = dx ? a.shape_dx : a.shape_dw;
+  a.planes == 3 ? grads<3>(a, piece, shape, dx, dw, st) : grads<1>(a, piece, shape, dx, dw, st);
   return hipGetLastError();
 }
 hipError_t launch_logprob_dx_sum(const LogprobArgs& a, hipStream_t st) {
@@ -1043,11 +1056,6 @@ hipError_t launch_logprob_dx_sum(const LogprobArgs& a, hipStream_t st) {
 hipError_t launch_logprob_dw_sum(const LogprobArgs& a, int piece, hipStream_t st) {
   const int64_t at = (int64_t)piece * a.piece_v * a.h * (a.planes == 3 ? 4 : 2);
   sum_slabs<false>(a, a.dw_acc, (int64_t)a.piece_v * a.h, a.splits_dw, (uint8_t*)a.dW + at, piece_rows(a, piece), st);
-  return hipGetLastError();
-}
-hipError_t launch_logprob_dw(const LogprobArgs& a, int piece, hipStream_t st) {
-  if (a.planes == 3) dw<3>(a, piece, st);
-  else dw<1>(a, piece, st);
   return hipGetLastError();
 }
 

@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -41,9 +42,9 @@ def check_hazards(src, extra_flags=None) -> None:
 
 def build(verbose: bool = False, extra_flags=None) -> str:
     """Compile every source for gfx950, check the kernels' MFMA hazards, link; returns the path."""
-    objs = []
     os.makedirs(os.path.join(PKG, "_build"), exist_ok=True)
-    for src in SOURCES:
+
+    def compile_one(src):
         obj = os.path.join(PKG, "_build", os.path.splitext(src)[0] + ".o")
         cmd = [HIPCC, f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-I", INCLUDE, "-I", CSRC,
                *DEVICE_FLAGS, *(extra_flags or []), "-c", os.path.join(CSRC, src), "-o", obj]
@@ -53,9 +54,12 @@ def build(verbose: bool = False, extra_flags=None) -> str:
         out = _run(cmd)
         if verbose and out.strip():
             print(out)
-        objs.append(obj)
         if src.endswith(".hip"):
             check_hazards(src, extra_flags)
+        return obj
+
+    with ThreadPoolExecutor(min(4, os.cpu_count() or 1)) as pool:
+        objs = list(pool.map(compile_one, SOURCES))
     tmp = LIB + ".tmp"
     _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs])
     os.replace(tmp, LIB)

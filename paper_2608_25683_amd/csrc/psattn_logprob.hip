@@ -20,7 +20,7 @@ using namespace dev;
 // of each of P planes, RING of them in LDS.
 //
 // Large, 8192 x 128256 logits of 4096: 6.30 ms, 1366 TFLOP/s (a library product of this kind: 1480).  Two wavefronts per SIMD, so
-// that one's products cover the other's waits.  Bound by power: the matrix cores are busy 71% of the cycles at 1.74 GHz
+// that one's products cover the other's waits.  Bound by power: the matrix cores are busy 71-77% of the cycles at 1.74-1.52 GHz
 // (2.13 with nothing else to do); without the copies 80% at 1.81, with data that is always in L2 73% at 1.78.  Tried and
 // slower: four wavefronts of 128 x 128 (7.07 ms, nothing covers a wait), stages of 32 in rings of 4 and 5 (6.8: twice the
 // barriers), raised wave priorities (no change).

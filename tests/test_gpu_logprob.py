@@ -187,7 +187,7 @@ def test_one_gradient_alone_is_the_same(dtype):
 
 
 def test_one_token_is_the_target_of_all_rows():
-    """More targets in one tile than its list holds at a time (4096 of them), and rows with hundreds of targets."""
+    """More targets in one tile than its list holds at a time, and rows with hundreds of targets."""
     n, h, v = 4500, 64, 300
     x, w, ptr, tgt, g = make(n, h, v, "bf16", 61, per_row=[1] * n)
     tgt[:] = 77

@@ -1352,19 +1352,23 @@ struct LogprobPlan {
 // one with its copies further ahead; parts are written and read as fp32 at 4.5 TB/s behind another launch.  (1280 rows x 1024 x 32000:
 // dX as 80 tiles of 500 stages 315, as seven parts 60; 512 rows x 4096 x 16000: logits 95 large, 67 small, as estimated.)
 struct LogprobTiling { int32_t shape, splits, stages; double us; };
-LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes, int max_splits, int shape = -1) {
+LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes, int max_splits, int shape = -1, bool logits = false) {
   struct Kind { int32_t shape, m, n, slots; double stage, ends; };
-  static const std::vector<Kind> bf16 = {{LP_LARGE, 256, 256, 256, 1.5, 10}, {LP_SMALL, 128, 128, 512, 0.83, 8}, {LP_DEEP, 128, 128, 256, 0.5, 8}};
-  static const std::vector<Kind> fp32 = {{LP_LARGE, 256, 128, 256, 4.1, 12}, {LP_SMALL, 128, 128, 256, 3.2, 10}};
+  static constexpr Kind bf16[] = {{LP_LARGE, 256, 256, 256, 1.5, 10}, {LP_SMALL, 128, 128, 512, 0.83, 8}, {LP_DEEP, 128, 128, 256, 0.5, 8}};
+  static constexpr Kind fp32[] = {{LP_LARGE, 256, 128, 256, 4.1, 12}, {LP_SMALL, 128, 128, 256, 3.2, 10}};
   LogprobTiling best{LP_LARGE, 1, 1, 1e30};
   const int64_t nk = std::max<int64_t>(1, (k + 63) / 64);
-  for (const Kind& c : planes == 3 ? fp32 : bf16) {
+  const Kind* kinds = planes == 3 ? fp32 : bf16;
+  for (int i = 0; i < (planes == 3 ? 2 : 3); ++i) {
+    const Kind& c = kinds[i];
     if (shape >= 0 && c.shape != shape) continue;
-    const int64_t tiles = ((down + c.m - 1) / c.m) * ((across + c.n - 1) / c.n);
+    const int64_t rest = across % c.n;
+    const bool narrow = logits && c.shape == LP_LARGE && rest > 0 && rest <= 64;   // (the logits' last rows: two fifths of a tile's time)
+    const double tiles = (double)((down + c.m - 1) / c.m) * ((double)((across + c.n - 1) / c.n) - (narrow ? 0.6 : 0));
     for (int64_t s = 1; s <= max_splits && s <= nk; ++s) {
       const int64_t each = (nk + s - 1) / s, parts = (nk + each - 1) / each;
       if (parts != s) continue;
-      const double r = (double)(tiles * s) / c.slots, rounds = std::ceil(r);
+      const double r = tiles * (double)s / c.slots, rounds = std::ceil(r);
       const double slabs = (double)s * (double)down * (double)across * 4;
       if (s > 1 && slabs > (double)((int64_t)512 << 20)) break;
       const double us = (rounds + std::max(r, 1.0)) / 2 * ((double)each * c.stage + c.ends) +
@@ -1409,7 +1413,7 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   // (a launch holds 2^32 threads, of at most 512 per tile of 128 x 128 and more; 128 x 32 ones have one row of tiles and 256)
   if ((int64_t)(a.n / 128 + 1) * (std::max(a.v, a.h) / 128 + 1) >= 1 << 23)
     return fail(PSATTN_E_UNSUPPORTED, "rows %d x vocab %d: more tiles than a launch holds", a.n, a.v);
-  a.shape = a.n <= 32 ? LP_THIN : logprob_tiling(std::min(a.v, a.piece_v), a.n, a.hp, a.planes, 1).shape;
+  a.shape = a.n <= 32 ? LP_THIN : logprob_tiling(std::min(a.v, a.piece_v), a.n, a.hp, a.planes, 1, -1, true).shape;
   a.part_v = a.shape == LP_LARGE ? 256 : 128;
   // The gradients' tiles of one shape, if that costs less than a tenth by the estimate: one launch then fills the chip for both.
   const int64_t pv = std::min(a.v, a.piece_v);

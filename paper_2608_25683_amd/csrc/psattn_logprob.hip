@@ -8,6 +8,7 @@
 // fp32 operands are three bf16 planes each, x = x1 + x2 + x3 exactly; a product takes the six pairs of planes whose
 // indices add up to at most 4, smallest first.  What is left out is below 2^-23 of a term, and 2^-25 of it on average.
 #include <algorithm>
+#include <type_traits>
 
 #include "psattn_device.h"
 
@@ -74,8 +75,10 @@ template <int BK>
 __device__ __forceinline__ int kswz(int i) { return BK == 64 ? (i >> 1) & 7 : (i >> 2) & 3; }
 template <int I, int BK, int WAVES, bool KOUTER>
 struct Loader {
-  static constexpr int COUNT = I * BK * 2 / 1024 / WAVES;
-  static_assert(COUNT * 1024 * WAVES == I * BK * 2, "whole instructions");
+  static constexpr int ALL = I * BK * 2 / 1024, COUNT = ALL < WAVES ? 1 : ALL / WAVES;   // instructions: of all wavefronts, of one
+  static_assert(ALL * 1024 == I * BK * 2 && (ALL < WAVES ? WAVES % ALL : ALL % WAVES) == 0, "whole instructions");
+  // the first one of a wavefront (where there are fewer than wavefronts, several copy the same)
+  static __device__ __forceinline__ int first(int wave) { return wave * COUNT % ALL; }
   const bf16_t* p;       // element (i0, 0) of the first plane
   int64_t step;          // bytes from one stage to the next
   uint32_t off[COUNT];   // of each instruction's lane, from the stage's first element
@@ -85,7 +88,7 @@ struct Loader {
     const int ilim = (int)min((int64_t)I, o.rows - i0);
 #pragma unroll
     for (int j = 0; j < COUNT; ++j) {
-      const int u = wave * COUNT + j;
+      const int u = first(wave) + j;
       if (KOUTER) {
         constexpr int per = I / 8;
         const int k = u * (64 / per) + lane / per;
@@ -182,8 +185,8 @@ __device__ __forceinline__ void product(f32x16 (&acc)[S::FM][S::FN], const Opera
       qa[q] = uniform((const char*)(la.p + q * A.plane) + ta * la.step);
       qb[q] = uniform((const char*)(lb.p + q * B.plane) + tb * lb.step);
     }
-    da = at + fill * S::STAGE + wave * LA::COUNT * 1024;
-    db = at + fill * S::STAGE + S::M * BK * 2 + wave * LB::COUNT * 1024;
+    da = at + fill * S::STAGE + LA::first(wave) * 1024;
+    db = at + fill * S::STAGE + S::M * BK * 2 + LB::first(wave) * 1024;
     if (++fill == S::RING) fill = 0;
     ++kt;
   };
@@ -492,21 +495,13 @@ __global__ __launch_bounds__(256) void wplanes_kernel(LogprobArgs a, int piece) 
 // addition and half a maximum per logit; nothing else is written.  Backward: dz of the tile, scaled, as bf16 or as
 // planes: 6.84 ms for 8192 x 128256 x 4096 (every row live) against the forward's 6.30, for the same product and 2 GB written.
 template <class S, bool BACKWARD>
-__global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs, int acrosses) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+__device__ __forceinline__ void logits_tile(const LogprobArgs& a, int piece, int np, int down_tile, int64_t j0, uint8_t* lds, LogprobRow* s_row) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int np = a.n, blocks = gridDim.x;
-  if (BACKWARD) {   // (fewer rows are live than the launch has room for)
-    np = up64(*a.live), acrosses = (np + S::N - 1) / S::N, blocks = downs * acrosses;
-    if ((int)blockIdx.x >= blocks) return;
-  }
-  const Tile tile = tile_of(blockIdx.x, blocks, downs, acrosses);
-  const int64_t i0 = (int64_t)tile.down * S::M, j0 = (int64_t)tile.across * S::N;
+  const int64_t i0 = (int64_t)down_tile * S::M;
   const int iw = (int)i0 + wave / S::WN * S::FM * 32, jw = wave % S::WN * S::FN * 32;   // the wavefront's first entry and row of the tile
   f32x16 acc[S::FM][S::FN];
   const Operand W = w_operand(a, piece);
-  __shared__ LogprobRow s_row[BACKWARD ? S::N : 1];        // (here so that its reads' time passes under the products)
-  if constexpr (BACKWARD)
+  if constexpr (BACKWARD)   // (here so that its reads' time passes under the products)
     for (int j = threadIdx.x; j < S::N; j += S::THREADS)
       if (j0 + j < np) s_row[j] = a.row[j0 + j];
   product<S, false, false>(acc, W, x_operand(a, np), i0, j0, a.hp, lds);
@@ -543,7 +538,7 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
       LogprobStat p = part[j];
 #pragma unroll
       for (int w = 1; w < S::WM; ++w) p = join(p, part[w * S::N + j]);
-      if (j0 + j < a.n) a.part[((int64_t)piece * a.piece_v / S::M + tile.down) * a.n + j0 + j] = p;
+      if (j0 + j < a.n) a.part[((int64_t)piece * a.piece_v / S::M + down_tile) * a.n + j0 + j] = p;
     }
     return;
   } else {
@@ -630,6 +625,31 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
             [&](int j) { return out + ((int64_t)Q * a.np + j) * a.piece_v; }, lim_across, lim_down, lds);
       });
     }
+  }
+}
+
+// Up to 64 rows behind the whole tiles of the largest kind have narrow ones, which start last and fill the compute units that
+// the whole ones leave idle: 777 rows x 1000 x 50257 126 us with whole tiles for the last 9 rows, 102 so; 320 rows 52 and
+// 44; 513 fp32 rows x 1024 x 16001 134 and 120; 64 rows x 4096 x 128256, bound by W's bytes, 227 and 224 (298 with each XCD's tiles
+// spread over all of W).  Smaller tiles gain nothing: 129 rows x 1024 x 32000 20 us, 23 so.
+template <class S>
+using TailOf = Tiling<S::WAVES / 2, 2, S::M / (16 * S::WAVES), 1, S::BK, S::LDS / ((S::M + 64) * S::BK * 2 * S::P), S::P>;
+template <class S, bool BACKWARD>
+__global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs) {
+  constexpr bool TAIL = S::WAVES == 8;
+  using T = std::conditional_t<TAIL, TailOf<S>, S>;
+  static_assert(T::M == S::M && T::THREADS == S::THREADS && T::LDS <= S::LDS, "in its place");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+  __shared__ LogprobRow s_row[BACKWARD ? S::N : 1];
+  const int np = BACKWARD ? up64(*a.live) : a.n;   // (fewer rows are live than the launch has room for)
+  int whole = (np + S::N - 1) / S::N;
+  if (TAIL && np - (whole - 1) * S::N <= T::N) --whole;
+  const int block = blockIdx.x, blocks = downs * whole;
+  if (block < blocks) {
+    const Tile tile = tile_of(block, blocks, downs, whole);
+    logits_tile<S, BACKWARD>(a, piece, np, tile.down, (int64_t)tile.across * S::N, lds, s_row);
+  } else if (TAIL && block < blocks + downs && whole * S::N < np) {
+    logits_tile<T, BACKWARD>(a, piece, np, tile_of(block - blocks, downs, downs, 1).down, (int64_t)whole * S::N, lds, s_row);
   }
 }
 
@@ -1001,7 +1021,7 @@ namespace {
 template <class S, bool BACKWARD>
 void launch_logits(const LogprobArgs& a, int piece, hipStream_t st) {
   const int d = tiles(piece_rows(a, piece), S::M), c = tiles(BACKWARD ? a.np : a.n, S::N);
-  hipLaunchKernelGGL((logits_kernel<S, BACKWARD>), dim3((unsigned)d * (unsigned)c), dim3(S::THREADS), 0, st, a, piece, d, c);
+  hipLaunchKernelGGL((logits_kernel<S, BACKWARD>), dim3((unsigned)d * (unsigned)c), dim3(S::THREADS), 0, st, a, piece, d);
 }
 template <int P, bool BACKWARD>
 void logits(const LogprobArgs& a, int piece, hipStream_t st) {

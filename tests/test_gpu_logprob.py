@@ -110,6 +110,14 @@ def test_against_the_definition(n, h, v, dtype):
     check(call(*a, scale=scale), *reference(*a, scale), f"{dtype} {n}x{h}x{v}")
 
 
+@pytest.mark.parametrize("dtype,n", [("bf16", 257), ("bf16", 320), ("bf16", 321), ("bf16", 590), ("bf16", 64), ("fp32", 129), ("fp32", 192),
+                                     ("fp32", 193), ("fp32", 300), ("fp32", 61)])
+def test_last_rows_before_a_large_vocabulary(dtype, n):
+    """Up to 64 rows behind the whole tiles of 256 (fp32: 128) have narrow ones; one row more, and these are whole too."""
+    a = make(n, 72, 24001, dtype, n, per_row=[1] * n)
+    check(call(*a), *reference(*a, 1.0), f"{dtype} {n}")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_rows_without_targets_and_targets_left_out(dtype):
     n, h, v = 70, 64, 300

@@ -634,17 +634,23 @@ __device__ __forceinline__ void logits_tile(const LogprobArgs& a, int piece, int
 // spread over all of W).  Smaller tiles gain nothing: 129 rows x 1024 x 32000 20 us, 23 so.
 template <class S>
 using TailOf = Tiling<S::WAVES / 2, 2, S::M / (16 * S::WAVES), 1, S::BK, S::LDS / ((S::M + 64) * S::BK * 2 * S::P), S::P>;
+template <class S>
+inline constexpr bool HasTail = S::WAVES == 8;
+// whole tiles of a row of them: the narrow one takes what is left
+template <class S>
+__device__ __forceinline__ int whole_tiles(int rows) {
+  const int n = (rows + S::N - 1) / S::N;
+  return HasTail<S> && n && rows - (n - 1) * S::N <= 64 ? n - 1 : n;
+}
 template <class S, bool BACKWARD>
 __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs) {
-  constexpr bool TAIL = S::WAVES == 8;
+  constexpr bool TAIL = HasTail<S>;
   using T = std::conditional_t<TAIL, TailOf<S>, S>;
   static_assert(T::M == S::M && T::THREADS == S::THREADS && T::LDS <= S::LDS, "in its place");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   __shared__ LogprobRow s_row[BACKWARD ? S::N : 1];
   const int np = BACKWARD ? up64(*a.live) : a.n;   // (fewer rows are live than the launch has room for)
-  int whole = (np + S::N - 1) / S::N;
-  if (TAIL && np - (whole - 1) * S::N <= T::N) --whole;
-  const int block = blockIdx.x, blocks = downs * whole;
+  const int whole = whole_tiles<S>(np), block = blockIdx.x, blocks = downs * whole;
   if (block < blocks) {
     const Tile tile = tile_of(block, blocks, downs, whole);
     logits_tile<S, BACKWARD>(a, piece, np, tile.down, (int64_t)tile.across * S::N, lds, s_row);
@@ -960,8 +966,17 @@ __global__ __launch_bounds__(S::THREADS) void grads_kernel(LogprobArgs a, int pi
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   const int block = blockIdx.x;
   if (block < dx_blocks) {
-    const int acrosses = (*a.live + S::N - 1) / S::N, blocks = downs * acrosses * a.splits_dx;
-    if (block < blocks) dx_tile<S>(a, piece, tile_of(block, blocks, downs, acrosses), lds);
+    constexpr bool TAIL = HasTail<S>;
+    using T = std::conditional_t<TAIL, TailOf<S>, S>;
+    static_assert(T::M == S::M && T::THREADS == S::THREADS && T::LDS <= S::LDS, "in its place");
+    const int live = *a.live, whole = whole_tiles<S>(live), parts = downs * a.splits_dx, blocks = parts * whole;
+    if (block < blocks) {
+      dx_tile<S>(a, piece, tile_of(block, blocks, downs, whole), lds);
+    } else if (TAIL && block < blocks + parts && whole * S::N < live) {
+      Tile tile = tile_of(block - blocks, parts, downs, 1);
+      tile.across = whole * (S::N / T::N);
+      dx_tile<T>(a, piece, tile, lds);
+    }
   } else {
     dw_tile<S>(a, piece, tile_of(block - dx_blocks, dw_blocks, downs, dw_acrosses), lds);
   }

@@ -1351,6 +1351,7 @@ struct LogprobPlan {
 // elements.  Measured: 1.5 a stage for 256 x 256 tiles, 0.83 for two workgroups of 128 x 128 per CU, 0.5 for
 // one with its copies further ahead; parts are written and read as fp32 at 4.5 TB/s behind another launch.  (1280 rows x 1024 x 32000:
 // dX as 80 tiles of 500 stages 315, as seven parts 60; 512 rows x 4096 x 16000: logits 95 large, 67 small, as estimated.)
+// by_rows: across are rows, of which up to 64 behind whole tiles of the largest kind have narrow ones.
 struct LogprobTiling { int32_t shape, splits, stages; double us; };
 LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes, int max_splits, int shape = -1, bool by_rows = false) {
   struct Kind { int32_t shape, m, n, slots; double stage, ends; };

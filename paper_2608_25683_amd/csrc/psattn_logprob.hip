@@ -629,9 +629,10 @@ __device__ __forceinline__ void logits_tile(const LogprobArgs& a, int piece, int
 }
 
 // Up to 64 rows behind the whole tiles of the largest kind have narrow ones, which start last and fill the compute units that
-// the whole ones leave idle: 777 rows x 1000 x 50257 126 us with whole tiles for the last 9 rows, 102 so; 320 rows 52 and
-// 44; 513 fp32 rows x 1024 x 16001 134 and 120; 64 rows x 4096 x 128256, bound by W's bytes, 227 and 224 (298 with each XCD's tiles
-// spread over all of W).  Smaller tiles gain nothing: 129 rows x 1024 x 32000 20 us, 23 so.
+// the whole ones leave idle: logits of 777 rows x 1000 x 50257 126 us with whole tiles for the last 9 rows, 102 so; 320 rows 52
+// and 44; 513 fp32 rows x 1024 x 16001 134 and 120; 64 rows x 4096 x 128256, bound by W's bytes, 227 and 222 (298 with each XCD's
+// tiles spread over all of W).  The same for dX: both gradients of 2080 rows x 1544 x 50257 696 us, 654 so.  Smaller tiles gain
+// nothing (logits of 129 rows x 1024 x 32000 20 us, 23 so).
 template <class S>
 using TailOf = Tiling<S::WAVES / 2, 2, S::M / (16 * S::WAVES), 1, S::BK, S::LDS / ((S::M + 64) * S::BK * 2 * S::P), S::P>;
 template <class S>

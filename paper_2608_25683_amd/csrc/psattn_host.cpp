@@ -1351,28 +1351,31 @@ struct LogprobPlan {
 // elements.  Measured: 1.5 a stage for 256 x 256 tiles, 0.83 for two workgroups of 128 x 128 per CU, 0.5 for
 // one with its copies further ahead; parts are written and read as fp32 at 4.5 TB/s behind another launch.  (1280 rows x 1024 x 32000:
 // dX as 80 tiles of 500 stages 315, as seven parts 60; 512 rows x 4096 x 16000: logits 95 large, 67 small, as estimated.)
-// by_rows: across are rows, of which up to 64 behind whole tiles of the largest kind have narrow ones.
+// Across may be rows, of which up to 64 behind whole tiles of the largest kind have narrow ones (of fp32 logits 128 entries down).
+enum class LogprobRows { none, logits, dx };
 struct LogprobTiling { int32_t shape, splits, stages; double us; };
-LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes, int max_splits, int shape = -1, bool by_rows = false) {
+LogprobTiling logprob_tiling(int64_t down, int64_t across, int64_t k, int planes, int max_splits, int shape = -1, LogprobRows rows = LogprobRows::none) {
   struct Kind { int32_t shape, m, n, slots; double stage, ends; };
   static constexpr Kind bf16[] = {{LP_LARGE, 256, 256, 256, 1.5, 10}, {LP_SMALL, 128, 128, 512, 0.83, 8}, {LP_DEEP, 128, 128, 256, 0.5, 8}};
   static constexpr Kind fp32[] = {{LP_LARGE, 256, 128, 256, 4.1, 12}, {LP_SMALL, 128, 128, 256, 3.2, 10}};
   LogprobTiling best{LP_LARGE, 1, 1, 1e30};
   const int64_t nk = std::max<int64_t>(1, (k + 63) / 64);
   const Kind* kinds = planes == 3 ? fp32 : bf16;
-  const double part = planes == 3 ? 0.65 : 0.4;   // a narrow tile's share of a whole one's time
+  const bool halves = planes == 3 && rows == LogprobRows::logits;
+  const double part = halves ? 0.35 : planes == 3 ? 0.65 : 0.4;   // a narrow tile's share of a whole one's time
   for (int i = 0; i < (planes == 3 ? 2 : 3); ++i) {
     const Kind& c = kinds[i];
     if (shape >= 0 && c.shape != shape) continue;
     const int64_t rest = across % c.n;
-    const bool narrow = by_rows && c.shape == LP_LARGE && rest > 0 && rest <= 64;
+    const bool narrow = rows != LogprobRows::none && c.shape == LP_LARGE && rest > 0 && rest <= 64;
     const int64_t downs = (down + c.m - 1) / c.m, whole = downs * ((across + c.n - 1) / c.n - narrow);
+    const int64_t tails = !narrow ? 0 : halves ? (down + 127) / 128 : downs;
     for (int64_t s = 1; s <= max_splits && s <= nk; ++s) {
       const int64_t each = (nk + s - 1) / s, parts = (nk + each - 1) / each;
       if (parts != s) continue;
-      const double full = std::ceil((double)(whole * s) / c.slots), r = ((double)(whole * s) + (narrow ? part * (double)(downs * s) : 0)) / c.slots;
+      const double full = std::ceil((double)(whole * s) / c.slots), r = ((double)(whole * s) + part * (double)(tails * s)) / c.slots;
       // (narrow tiles run beside the last whole ones as far as there is room, then by themselves)
-      const double behind = narrow ? std::ceil(std::max(0.0, (double)((whole + downs) * s) / c.slots - full)) * part : 0, rounds = full + behind;
+      const double behind = std::ceil(std::max(0.0, (double)((whole + tails) * s) / c.slots - full)) * part, rounds = full + behind;
       const double slabs = (double)s * (double)down * (double)across * 4;
       if (s > 1 && slabs > (double)((int64_t)512 << 20)) break;
       const double us = (rounds + std::max(r, 1.0)) / 2 * ((double)each * c.stage + c.ends) +
@@ -1417,15 +1420,15 @@ psattn_status logprob_plan(const psattn_logprob_desc* d, int pass, LogprobPlan& 
   // (a launch holds 2^32 threads, of at most 512 per tile of 128 x 128 and more; 128 x 32 ones have one row of tiles and 256)
   if ((int64_t)(a.n / 128 + 1) * (std::max(a.v, a.h) / 128 + 1) >= 1 << 23)
     return fail(PSATTN_E_UNSUPPORTED, "rows %d x vocab %d: more tiles than a launch holds", a.n, a.v);
-  a.shape = a.n <= 32 ? LP_THIN : logprob_tiling(std::min(a.v, a.piece_v), a.n, a.hp, a.planes, 1, -1, true).shape;
-  a.part_v = a.shape == LP_LARGE ? 256 : 128;
+  a.shape = a.n <= 32 ? LP_THIN : logprob_tiling(std::min(a.v, a.piece_v), a.n, a.hp, a.planes, 1, -1, LogprobRows::logits).shape;
+  a.part_v = a.shape == LP_LARGE && !fp32 ? 256 : 128;
   // The gradients' tiles of one shape, if that costs less than a tenth by the estimate: one launch then fills the chip for both.
   const int64_t pv = std::min(a.v, a.piece_v);
-  LogprobTiling dx = logprob_tiling(a.h, a.n, pv, a.planes, 32, -1, true), dw = logprob_tiling(a.h, pv, a.n, a.planes, 32);
+  LogprobTiling dx = logprob_tiling(a.h, a.n, pv, a.planes, 32, -1, LogprobRows::dx), dw = logprob_tiling(a.h, pv, a.n, a.planes, 32);
   double most = 1.1 * (dx.us + dw.us);
   for (int shape : {LP_LARGE, LP_SMALL, LP_DEEP}) {
     if (fp32 && shape == LP_DEEP) continue;
-    const LogprobTiling x = logprob_tiling(a.h, a.n, pv, a.planes, 32, shape, true), w = logprob_tiling(a.h, pv, a.n, a.planes, 32, shape);
+    const LogprobTiling x = logprob_tiling(a.h, a.n, pv, a.planes, 32, shape, LogprobRows::dx), w = logprob_tiling(a.h, pv, a.n, a.planes, 32, shape);
     if (x.us + w.us < most) most = x.us + w.us, dx = x, dw = w;
   }
   a.shape_dx = dx.shape, a.splits_dx = dx.splits, a.stages_dx = dx.stages;

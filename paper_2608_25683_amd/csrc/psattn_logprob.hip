@@ -535,10 +535,14 @@ __device__ __forceinline__ void logits_tile(const LogprobArgs& a, int piece, int
     }
     __syncthreads();
     for (int j = threadIdx.x; j < S::N; j += S::THREADS) {
-      LogprobStat p = part[j];
+      constexpr int PART = S::P == 3 ? 128 : S::M, WAVES = S::WM * PART / S::M;   // entries of a part, wavefronts down it
 #pragma unroll
-      for (int w = 1; w < S::WM; ++w) p = join(p, part[w * S::N + j]);
-      if (j0 + j < a.n) a.part[((int64_t)piece * a.piece_v / S::M + down_tile) * a.n + j0 + j] = p;
+      for (int k = 0; k < S::M / PART; ++k) {
+        LogprobStat p = part[k * WAVES * S::N + j];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) p = join(p, part[(k * WAVES + w) * S::N + j]);
+        if (j0 + j < a.n && i0 + k * PART < W.rows) a.part[((piece * (int64_t)a.piece_v + i0) / PART + k) * a.n + j0 + j] = p;
+      }
     }
     return;
   } else {
@@ -630,11 +634,16 @@ __device__ __forceinline__ void logits_tile(const LogprobArgs& a, int piece, int
 
 // Up to 64 rows behind the whole tiles of the largest kind have narrow ones, which start last and fill the compute units that
 // the whole ones leave idle: logits of 777 rows x 1000 x 50257 126 us with whole tiles for the last 9 rows, 102 so; 320 rows 52
-// and 44; 513 fp32 rows x 1024 x 16001 134 and 120; 64 rows x 4096 x 128256, bound by W's bytes, 227 and 222 (298 with each XCD's
+// and 44; 513 fp32 rows x 1024 x 16001 134 and 104; 64 rows x 4096 x 128256, bound by W's bytes, 227 and 222 (298 with each XCD's
 // tiles spread over all of W).  The same for dX: both gradients of 2080 rows x 1544 x 50257 696 us, 654 so.  Smaller tiles gain
-// nothing (logits of 129 rows x 1024 x 32000 20 us, 23 so).
+// nothing (logits of 129 rows x 1024 x 32000 20 us, 23 so).  fp32 logits: half as many entries, twice as long stages, so that
+// whole 128 bytes of a row are copied at a time (513 rows: 118 us otherwise).
+template <class S, int M, int BK>
+using Narrow = Tiling<S::WAVES / 2, 2, M / (16 * S::WAVES), 1, BK, S::LDS / ((M + 64) * BK * 2 * S::P), S::P>;
 template <class S>
-using TailOf = Tiling<S::WAVES / 2, 2, S::M / (16 * S::WAVES), 1, S::BK, S::LDS / ((S::M + 64) * S::BK * 2 * S::P), S::P>;
+using LogitsTail = Narrow<S, S::P == 3 ? 128 : S::M, 64>;
+template <class S>
+using GradsTail = Narrow<S, S::M, S::BK>;
 template <class S>
 inline constexpr bool HasTail = S::WAVES == 8;
 // whole tiles of a row of them: the narrow one takes what is left
@@ -644,10 +653,10 @@ __device__ __forceinline__ int whole_tiles(int rows) {
   return HasTail<S> && n && rows - (n - 1) * S::N <= 64 ? n - 1 : n;
 }
 template <class S, bool BACKWARD>
-__global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs) {
+__global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int piece, int downs, int tails) {
   constexpr bool TAIL = HasTail<S>;
-  using T = std::conditional_t<TAIL, TailOf<S>, S>;
-  static_assert(T::M == S::M && T::THREADS == S::THREADS && T::LDS <= S::LDS, "in its place");
+  using T = std::conditional_t<TAIL, LogitsTail<S>, S>;
+  static_assert(T::THREADS == S::THREADS && T::LDS <= S::LDS, "in its place");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
   __shared__ LogprobRow s_row[BACKWARD ? S::N : 1];
   const int np = BACKWARD ? up64(*a.live) : a.n;   // (fewer rows are live than the launch has room for)
@@ -655,8 +664,8 @@ __global__ __launch_bounds__(S::THREADS) void logits_kernel(LogprobArgs a, int p
   if (block < blocks) {
     const Tile tile = tile_of(block, blocks, downs, whole);
     logits_tile<S, BACKWARD>(a, piece, np, tile.down, (int64_t)tile.across * S::N, lds, s_row);
-  } else if (TAIL && block < blocks + downs && whole * S::N < np) {
-    logits_tile<T, BACKWARD>(a, piece, np, tile_of(block - blocks, downs, downs, 1).down, (int64_t)whole * S::N, lds, s_row);
+  } else if (TAIL && block < blocks + tails && whole * S::N < np) {
+    logits_tile<T, BACKWARD>(a, piece, np, tile_of(block - blocks, tails, tails, 1).down, (int64_t)whole * S::N, lds, s_row);
   }
 }
 
@@ -968,9 +977,9 @@ __global__ __launch_bounds__(S::THREADS) void grads_kernel(LogprobArgs a, int pi
   const int block = blockIdx.x;
   if (block < dx_blocks) {
     constexpr bool TAIL = HasTail<S>;
-    using T = std::conditional_t<TAIL, TailOf<S>, S>;
-    static_assert(T::M == S::M && T::THREADS == S::THREADS && T::LDS <= S::LDS, "in its place");
-    const int live = *a.live, whole = whole_tiles<S>(live), parts = downs * a.splits_dx, blocks = parts * whole;
+    using T = std::conditional_t<TAIL, GradsTail<S>, S>;
+    static_assert(T::THREADS == S::THREADS && T::LDS <= S::LDS, "in its place");
+    const int live = *a.live, whole = whole_tiles<S>(live), blocks = downs * a.splits_dx * whole, parts = downs * a.splits_dx;
     if (block < blocks) {
       dx_tile<S>(a, piece, tile_of(block, blocks, downs, whole), lds);
     } else if (TAIL && block < blocks + parts && whole * S::N < live) {
@@ -1033,11 +1042,17 @@ hipError_t launch_logprob_wplanes(const LogprobArgs& a, int piece, hipStream_t s
   return hipGetLastError();
 }
 namespace {
-// One workgroup per tile of down x across.
+// narrow tiles that cover n down
+template <class S>
+int tail_tiles(int64_t n) {
+  if constexpr (HasTail<S>) return tiles(n, LogitsTail<S>::M);
+  return 0;
+}
+// One workgroup per tile of down x across; of narrow ones there may be more down.
 template <class S, bool BACKWARD>
 void launch_logits(const LogprobArgs& a, int piece, hipStream_t st) {
-  const int d = tiles(piece_rows(a, piece), S::M), c = tiles(BACKWARD ? a.np : a.n, S::N);
-  hipLaunchKernelGGL((logits_kernel<S, BACKWARD>), dim3((unsigned)d * (unsigned)c), dim3(S::THREADS), 0, st, a, piece, d);
+  const int d = tiles(piece_rows(a, piece), S::M), c = tiles(BACKWARD ? a.np : a.n, S::N), tails = tail_tiles<S>(piece_rows(a, piece));
+  hipLaunchKernelGGL((logits_kernel<S, BACKWARD>), dim3((unsigned)d * (unsigned)c + (unsigned)std::max(0, tails - d)), dim3(S::THREADS), 0, st, a, piece, d, tails);
 }
 template <int P, bool BACKWARD>
 void logits(const LogprobArgs& a, int piece, hipStream_t st) {
